@@ -56,6 +56,14 @@ extern "C" {
 #define IM_STATUS_OVER_BUDGET 8     /* im_decode_step: a unit entered with len > budget; only one
                                        entry was evicted from it                                  */
 
+#define IM_STATUS_OUT_OF_PAGES 16       /* the page pool ran out: the units that got no pages were left as they were */
+#define IM_STATUS_BAD_FORK 32           /* im_fork_packed: a sequence's source is none, or does not stay; the sequence
+                                       was left as it was                                        */
+#define IM_STATUS_BAD_PAGE 64           /* a live slot's table entry names no page, or a list names no live slot: it was
+                                       skipped                                                   */
+#define IM_STATUS_BAD_LISTS 128         /* im_compact_packed: n_keep + n_evict is not the unit's length; it was left as
+                                       it was                                                    */
+
 typedef struct im_handle im_handle; /* opaque: validated config + workspace pointer, host memory */
 
 /* Shape of one layer's state and the method's constants. */
@@ -108,6 +116,33 @@ typedef struct im_state {
   float* M;             /* [B, H_kv, d_mem, d_head] fp32 fast weights                        */
   float* b;             /* [B, H_kv, d_mem]         fp32 stabiliser                          */
 } im_state;
+
+/* A cache whose K and V rows are held in 4 bits, in pages (device pointers, read and written in place).  It goes with
+ * an im_state whose K and V are not used (NULL): Kidx, pos, len, n_projected, M and b are as there, im_index_score and
+ * im_topb_select take that state as it is.  head_shared = 0 only.
+ *   A row of 128 values is 128 codes of 4 bits (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one scale byte s per 32 values:
+ * value = code * 2^(s - 127), with the smallest s in 1..254 for which no |value| of the 32 is above 6 * 2^(s - 127); each is
+ * rounded to the nearest code, ties to the even one (the larger of 0.5 and 1, of 1.5 and 2, of 3 and 4; else the smaller); what
+ * would be 2^128 is 3 * 2^126, the largest that bf16 holds.  A block
+ * with an infinity or a NaN reads as NaN (s = 255).
+ *   A page holds IM_PAGE_SLOTS slots of one unit in IM_PAGE_BYTES bytes: K codes (row r at 64 r; dim d in the low half of
+ * byte d / 2 for even d, else in the high half), V codes (8 dims 8 w .. 8 w + 7 of row r: the 4 bytes at 4096 +
+ * 1024 (r / 16) + 16 (16 (r % 16 / 4) + w) + 4 (r % 4)), K's scales (dims 32 c .. 32 c + 31 of row r: byte 8192 + 4 r + c), V's
+ * scales (byte 8448 + 64 (r / 16) + 16 (r % 16 / 4) + 4 c + r % 4).  136 bytes per entry, where bf16 rows take 512.
+ *   Slot i of a unit lies in row i % IM_PAGE_SLOTS of page table[b, h, i / IM_PAGE_SLOTS].  Units may hold pages together
+ * (im_fork_packed); refs counts a page's holders, 0 is a free page.  A call that writes to a page that others hold too takes a
+ * new one and copies it first.  A new pool has refs 0 and table -1 everywhere.  New pages are the free ones of the lowest
+ * numbers, in the order of the units and their slots.
+ *   The caller may set a len (and n_projected) to a smaller value, e.g. to drop rejected draft tokens: pages behind it
+ * stay with the unit, and later appends fill them. */
+#define IM_PAGE_SLOTS 64
+#define IM_PAGE_BYTES 8704
+typedef struct im_packed {
+  void* pages;          /* [n_pages, IM_PAGE_BYTES], 16-byte aligned                          */
+  int32_t* refs;        /* [n_pages] units that hold the page                                 */
+  int32_t* table;       /* [B, H_kv, ceil(C / IM_PAGE_SLOTS)] page, or -1                     */
+  int32_t n_pages;
+} im_packed;
 
 /* Bytes of workspace a handle for `cfg` needs (0 if cfg is invalid).  Host only. */
 size_t im_workspace_bytes(const im_config* cfg);
@@ -163,6 +198,7 @@ int32_t im_append_kv_hidden(im_handle* h, const im_params* p, const im_state* st
  * q_new [B, n_q, H, d_head] bf16; x_gate [B, n_q, gate_in_dim] bf16; q_pos [B, n_q] int32;
  * scores_out [B, H_kv, C] fp32, written for slots < len only.  1 <= n_q <= max_queries.
  * All arithmetic that feeds the stored bf16 / fp32 values is fp64.
+ * st->K = NULL (a cache in 4 bits; its keys were projected at the append): (i) is skipped.
  * head_shared = 1: (i) is skipped (the keys were made at the append), x_gate holds the queries'
  * hidden states, and scores_out is [B, C]: one score per token of the sequence. */
 int32_t im_index_score(im_handle* h, const im_params* p, const im_state* st, const void* q_new,
@@ -305,6 +341,50 @@ int32_t im_decode_step_shared_hidden(im_handle* h, const im_params* p, const im_
                                      const void* x_new, const void* k_new, const void* v_new,
                                      const int32_t* pos_new, const int32_t* evict_slot, float lambda,
                                      float eta, void* out, float* readout_dbg, void* stream);
+
+/* ---- the cache held in 4 bits, in pages (im_packed) --------------------------------------------------------------
+ * A step on it is
+ *     im_append_packed -> im_index_score -> im_topb_select -> im_unpack_kv (evicted rows) -> im_memory_update
+ *                      -> im_compact_packed -> im_attn_packed_with_readout
+ * where im_memory_update takes a state with the K, V that im_unpack_kv wrote to (buffers of one layer's size, which all layers
+ * can share) and the M, b of the cache's own.
+ * All of these calls return IM_ERR_UNSUPPORTED for head_shared = 1. */
+
+/* New tokens enter the cache: the rows k_new, v_new [B, H_kv, n_new, d_head] (bf16) go, rounded to 4 bits, to slots
+ * [len, len + n_new) of every unit, pos_new [B, n_new] to their positions, and Kidx = bf16(RMSNorm(Uk k_new)) (fp64 arithmetic,
+ * from the rows as given) to their indexer keys; len and n_projected become len + n_new.  1 <= n_new <= capacity.
+ * A unit with len + n_new > capacity is left unchanged (IM_STATUS_APPEND_OVERFLOW), and so is one whose new pages are not all
+ * among the free ones, counted in the order of the units (IM_STATUS_OUT_OF_PAGES). */
+int32_t im_append_packed(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* k_new,
+                         const void* v_new, const int32_t* pos_new, int32_t n_new, void* stream);
+
+/* Entries are read back: for the slots listed in idx [B, H_kv, C] (the first n_idx [B, H_kv] of each unit; e.g. evict_idx and
+ * n_evict of im_topb_select; both NULL: all of a unit's entries) the rows go, as bf16, to the SAME slots of K_out, V_out
+ * [B, H_kv, C, d_head].  Exact: every value of the 4-bit rows is a bf16 value.  Other rows are left as they are, and
+ * listed slots outside [0, len) are skipped. */
+int32_t im_unpack_kv(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* idx, const int32_t* n_idx, void* K_out,
+                     void* V_out, void* stream);
+
+/* Attention over the cache plus the gated memory readout, as im_decode_attn_with_readout has it, for n_q >= 1 queries per
+ * sequence: query s sees the entries with pos <= q_pos[b, s] (q_pos NULL: all of them); one that sees none has o_attn = 0.
+ * q, out [B, n_q, H, d_head] bf16; q_pos [B, n_q] int32 or NULL; readout_dbg [B, n_q, H, d_head] fp32 or NULL.
+ * For a chunk of a prompt: append its tokens, then attend with their positions.  A key or value block that reads as NaN makes
+ * NaN of the outputs of the queries that see it, and of no others.  batch * n_q * H < 2^31. */
+int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* q,
+                                    const int32_t* q_pos, int32_t n_q, void* out, float* readout_dbg, void* stream);
+
+/* im_compact_kv for this cache: kept entries in slots >= n_keep move into the evicted slots < n_keep, both in ascending order
+ * (their codes as they are); len = n_projected = n_keep; pages behind the last kept entry are given up.  A shared page that gets
+ * entries is copied first; a unit whose copies are not all among the free pages is left as it was (IM_STATUS_OUT_OF_PAGES).  Pages that
+ * the call gives up are free for the calls after it. */
+int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* keep_idx, const int32_t* n_keep,
+                          const int32_t* evict_idx, const int32_t* n_evict, void* stream);
+
+/* Sequences fork, and end: src_of [B] int32.  src_of[b] = b: sequence b stays as it is.  src_of[b] = a, with src_of[a] = a: b
+ * becomes a copy of a; the pages are held by both, Kidx, pos, M and b are copied, and what b held before is given up.
+ * src_of[b] = -1: b is emptied (len 0, no pages, M and b zero).  Anything else leaves sequence b as it is
+ * (IM_STATUS_BAD_FORK).  (A reordering of candidates is of this kind: those that live on stay where they are.) */
+int32_t im_fork_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* src_of, void* stream);
 
 /* Measurement only (not part of the method): one launch that reads `bytes` (a multiple of 16) from
  * src (device, 16-byte aligned) with 16-byte streaming loads on all CUs and writes nothing, unless the

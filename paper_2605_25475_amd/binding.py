@@ -17,13 +17,15 @@ from . import build as _build
 
 IM_OK, IM_ERR_INVALID_ARG, IM_ERR_UNSUPPORTED, IM_ERR_LAUNCH = 0, -1, -2, -3
 IM_STATUS_APPEND_OVERFLOW, IM_STATUS_LIVE_EXCEEDED, IM_STATUS_OVER_BUDGET = 1, 2, 8
+IM_STATUS_OUT_OF_PAGES, IM_STATUS_BAD_FORK, IM_STATUS_BAD_PAGE, IM_STATUS_BAD_LISTS = 16, 32, 64, 128
 IM_STATIC_SCRATCH_BYTES = 16 << 20
+IM_PAGE_SLOTS, IM_PAGE_BYTES = 64, 8704
 
 EXPORTS = [
     "im_workspace_bytes", "im_create", "im_destroy", "im_last_error", "im_set_max_live",
     "im_query_status", "im_append_kv", "im_append_kv_hidden", "im_index_score", "im_topb_select", "im_memory_update",
     "im_compact_kv", "im_gather_kept", "im_decode_attn_with_readout", "im_decode_attn_with_readout_static", "im_decode_step", "im_attend_step", "im_attend_step_hidden", "im_decode_step_shared", "im_decode_step_shared_hidden", "im_stream_read", "im_profile_start",
-    "im_profile_stop",
+    "im_profile_stop", "im_append_packed", "im_unpack_kv", "im_attn_packed_with_readout", "im_compact_packed", "im_fork_packed",
 ]
 
 
@@ -41,6 +43,10 @@ class ImParams(C.Structure):
 
 class ImState(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("K", "V", "Kidx", "pos", "len", "n_projected", "M", "b")]
+
+
+class ImPacked(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pages", "refs", "table")] + [("n_pages", C.c_int32)]
 
 
 class IndexMemError(RuntimeError):
@@ -114,6 +120,17 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.im_profile_start.argtypes = [vp, i32, i32]
     lib.im_profile_stop.restype = i32
     lib.im_profile_stop.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(i32), vp]
+    st, pk = C.POINTER(ImState), C.POINTER(ImPacked)
+    lib.im_append_packed.restype = i32
+    lib.im_append_packed.argtypes = [vp, C.POINTER(ImParams), st, pk, vp, vp, vp, i32, vp]
+    lib.im_unpack_kv.restype = i32
+    lib.im_unpack_kv.argtypes = [vp, st, pk, vp, vp, vp, vp, vp]
+    lib.im_attn_packed_with_readout.restype = i32
+    lib.im_attn_packed_with_readout.argtypes = [vp, C.POINTER(ImParams), st, pk, vp, vp, i32, vp, vp, vp]
+    lib.im_compact_packed.restype = i32
+    lib.im_compact_packed.argtypes = [vp, st, pk, vp, vp, vp, vp, vp]
+    lib.im_fork_packed.restype = i32
+    lib.im_fork_packed.argtypes = [vp, st, pk, vp, vp]
     _lib = lib
     return lib
 
@@ -189,6 +206,39 @@ class State:
         self.b = torch.zeros(S + (cfg.mem_dim,), dtype=torch.float32, **z)
         self.c = ImState(*(_ptr(t) for t in (self.K, self.V, self.Kidx, self.pos, self.len,
                                              self.n_projected, self.M, self.b)))
+
+
+class PackedState:
+    """State of one layer whose keys and values are held in 4 bits, in pages (im_packed): the pool of pages, its table and
+    counts, and the dense arrays of State but K and V.  Device tensors."""
+
+    def __init__(self, cfg: Config, n_pages: int, device="cuda"):
+        S, Cc = cfg.set_shape(), cfg.capacity
+        z = dict(device=device)
+        self.n_pages = n_pages
+        self.pages = torch.zeros((n_pages, IM_PAGE_BYTES), dtype=torch.uint8, **z)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, **z)
+        self.table = torch.full((cfg.batch, cfg.n_kv_heads, (Cc + IM_PAGE_SLOTS - 1) // IM_PAGE_SLOTS), -1, dtype=torch.int32, **z)
+        self.Kidx = torch.zeros(S + (Cc, cfg.idx_dim), dtype=torch.bfloat16, **z)
+        self.pos = torch.zeros(S + (Cc,), dtype=torch.int32, **z)
+        self.len = torch.zeros(S, dtype=torch.int32, **z)
+        self.n_projected = torch.zeros(S, dtype=torch.int32, **z)
+        self.M = torch.zeros(S + (cfg.mem_dim, cfg.head_dim), dtype=torch.float32, **z)
+        self.b = torch.zeros(S + (cfg.mem_dim,), dtype=torch.float32, **z)
+        self.c = ImState(None, None, *(_ptr(t) for t in (self.Kidx, self.pos, self.len, self.n_projected, self.M, self.b)))
+        self.pk = ImPacked(_ptr(self.pages), _ptr(self.refs), _ptr(self.table), n_pages)
+
+    def with_rows(self, K, V) -> "StateView":
+        """This state with the bf16 rows of K, V [B, H_kv, C, d_head]: what im_memory_update takes after im_unpack_kv."""
+        return StateView(self, K, V)
+
+
+class StateView:
+    """The dense arrays of a PackedState with K and V buffers of the caller's (it keeps them alive)."""
+
+    def __init__(self, st: PackedState, K, V):
+        self.parts = (st, K, V)
+        self.c = ImState(_ptr(K), _ptr(V), *(_ptr(t) for t in (st.Kidx, st.pos, st.len, st.n_projected, st.M, st.b)))
 
 
 class Handle:
@@ -320,6 +370,31 @@ def im_decode_step_shared_hidden(h: Handle, p: Params, st: State, q, x_new, k_ne
     h.check(h.lib.im_decode_step_shared_hidden(h.h, C.byref(p.c), C.byref(st.c), _ptr(q), _ptr(x_new), _ptr(k_new),
                                                _ptr(v_new), _ptr(pos_new), _ptr(evict_slot), lam, eta, _ptr(out),
                                                _ptr(readout_dbg), _stream()))
+
+
+def im_append_packed(h: Handle, p: Params, st: PackedState, k_new, v_new, pos_new) -> None:
+    h.check(h.lib.im_append_packed(h.h, C.byref(p.c), C.byref(st.c), C.byref(st.pk), _ptr(k_new), _ptr(v_new), _ptr(pos_new),
+                                   pos_new.shape[1], _stream()))
+
+
+def im_unpack_kv(h: Handle, st: PackedState, K_out, V_out, idx=None, n_idx=None) -> None:
+    h.check(h.lib.im_unpack_kv(h.h, C.byref(st.c), C.byref(st.pk), _ptr(idx), _ptr(n_idx), _ptr(K_out), _ptr(V_out), _stream()))
+
+
+def im_attn_packed_with_readout(h: Handle, p: Params, st: PackedState, q, out, q_pos=None, readout_dbg=None) -> None:
+    """q, out [B, n_q, H, d_head] (or [B, H, d_head] for one query per sequence)."""
+    n_q = q.shape[1] if q.dim() == 4 else 1
+    h.check(h.lib.im_attn_packed_with_readout(h.h, C.byref(p.c), C.byref(st.c), C.byref(st.pk), _ptr(q), _ptr(q_pos), n_q, _ptr(out),
+                                              _ptr(readout_dbg), _stream()))
+
+
+def im_compact_packed(h: Handle, st: PackedState, keep_idx, n_keep, evict_idx, n_evict) -> None:
+    h.check(h.lib.im_compact_packed(h.h, C.byref(st.c), C.byref(st.pk), _ptr(keep_idx), _ptr(n_keep), _ptr(evict_idx), _ptr(n_evict),
+                                    _stream()))
+
+
+def im_fork_packed(h: Handle, st: PackedState, src_of) -> None:
+    h.check(h.lib.im_fork_packed(h.h, C.byref(st.c), C.byref(st.pk), _ptr(src_of), _stream()))
 
 
 def im_stream_read(src: torch.Tensor, nbytes: int, never: int, sink: torch.Tensor) -> None:

@@ -1,0 +1,960 @@
+// The cache held in 4 bits, in pages: append, read back, attention with the memory readout, compaction, forks.
+//
+// A page holds IM_PAGE_SLOTS slots of one unit (batch element, KV head).  A row of 128 values is 128 codes of 4 bits (E2M1: sign and
+// 0, 0.5, 1, 1.5, 2, 3, 4, 6; even dims in the low halves of the bytes) and one scale byte s per 32 dims: value = code 2^(s - 127).
+// s = 255 marks a block that held an infinity or a NaN: all of it reads as NaN.  This is what the conversions and the scaled
+// products of gfx950 take: a scale byte shifted to a float's exponent is their scale operand, 255 included.
+//   bytes    0 .. 4095   K: row r at 64 r
+//         4096 .. 8191   V: word w (dims 8 w .. 8 w + 7) of row r at 1024 (r / 16) + 16 (16 (r % 16 / 4) + w) + 4 (r % 4): a lane's
+//                        share of 16 keys, 4 keys x 8 dims as the product P V takes them, is one 16-byte load
+//         8192 .. 8447   K scales: block c of row r at 4 r + c
+//         8448 .. 8703   V scales: block c of row r at 64 (r / 16) + 16 (r % 16 / 4) + 4 c + r % 4
+#pragma once
+#include "im_kernels.h"
+
+#define PG_SLOTS 64
+#define PG_BYTES 8704
+#define PG_V 4096
+#define PG_KS 8192
+#define PG_VS 8448
+#define IM_STATUS_OUT_OF_PAGES_BIT 16
+#define IM_STATUS_BAD_FORK_BIT 32
+#define IM_STATUS_BAD_PAGE_BIT 64
+#define IM_STATUS_BAD_LISTS_BIT 128
+
+typedef __bf16 im_bf2 __attribute__((ext_vector_type(2)));
+typedef float im_f2 __attribute__((ext_vector_type(2)));
+typedef float im_c16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ int pg_v_word(int r, int w) { return PG_V + (r >> 4) * 1024 + (((r & 15) >> 2) * 16 + w) * 16 + (r & 3) * 4; }
+__device__ __forceinline__ int pg_v_scale(int r, int c) { return PG_VS + (r >> 4) * 64 + ((r & 15) >> 2) * 16 + c * 4 + (r & 3); }
+__device__ __forceinline__ bool pg_is_page(int id, int n_pages) { return (uint32_t)id < (uint32_t)n_pages; }
+__device__ __forceinline__ float pg_scale(uint32_t s) { return __uint_as_float(s << 23); }
+
+// 8 codes -> 8 bf16 values
+__device__ __forceinline__ uint4 pg_expand(uint32_t w, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+}
+
+// 8 bf16 values per lane, 4 lanes (a quad) per block of 32 -> this lane's code word; s: the block's scale byte.
+// s is the smallest with |x| <= 6 * 2^(s - 127) for the whole block (s >= 1): nothing is clipped.  With |x| = 1.m 2^e that is
+// e - 2, and one more where 1.m > 1.5.  Codes are rounded to the nearest, ties to the even code.
+__device__ __forceinline__ uint32_t pg_quantise(uint4 x, uint32_t& s) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a = max(a, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0xB1, 0xF, 0xF, false));   // quad_perm 1 0 3 2
+  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
+  const int e = (int)(a >> 7) - 2 + ((a & 0x7f) > 0x40);
+  s = a >= 0x7f80u ? 255u : (uint32_t)max(e, 1);
+  const float f = pg_scale(s);
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(w[i]); v[2 * i + 1] = bf_hi(w[i]); }
+  if (s == 253u) {   // 4 * 2^126 is no bf16 value: what is nearest to it goes to 3 * 2^126
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fminf(fmaxf(v[i], -0x1.8p127f), 0x1.8p127f);
+  }
+  uint32_t q = 0;
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0], v[1], f, 0);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2], v[3], f, 1);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4], v[5], f, 2);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6], v[7], f, 3);
+  return s == 255u ? 0u : q;
+}
+
+// word k of 34 (16 of K, 16 of V, K's scales, V's scales) of a row, from one page's row to another's
+__device__ __forceinline__ void pg_copy_word(const char* src, int rs, char* dst, int rd, int k) {
+  if (k < 16) *(uint32_t*)(dst + rd * 64 + 4 * k) = *(const uint32_t*)(src + rs * 64 + 4 * k);
+  else if (k < 32) *(uint32_t*)(dst + pg_v_word(rd, k - 16)) = *(const uint32_t*)(src + pg_v_word(rs, k - 16));
+  else if (k == 32) *(uint32_t*)(dst + PG_KS + 4 * rd) = *(const uint32_t*)(src + PG_KS + 4 * rs);
+  else if (k == 33) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) dst[pg_v_scale(rd, c)] = src[pg_v_scale(rs, c)];
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// pages: who needs one, and which are free
+// ------------------------------------------------------------------------------------------
+// exclusive sum over the 1024 threads of a workgroup; total in every thread.  Every thread calls it.
+__device__ __forceinline__ int pg_scan(int v, int* s_wave, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int inc = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(inc, d, 64);
+    if (lane >= d) inc += o;
+  }
+  __syncthreads();   // (s_wave of the call before has been read)
+  if (lane == 63) s_wave[w] = inc;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int t = s_wave[i];
+    before += i < w ? t : 0;
+    total += t;
+  }
+  return before + inc - v;
+}
+
+// The lowest `want` free pages (refs = 0), ascending, to ids; returns how many there are of them.  One workgroup.
+__device__ __forceinline__ int pg_find_free(const int32_t* __restrict__ refs, int n_pages, int want, int32_t* ids, int* s_wave) {
+  int found = 0;
+  for (int p0 = 0; p0 < n_pages && found < want; p0 += 4096) {
+    const int p = p0 + 4 * threadIdx.x;
+    bool f[4];
+    int c = 0, total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = p + i < n_pages && refs[p + i] == 0;
+      c += f[i];
+    }
+    int at = found + pg_scan(c, s_wave, total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (f[i]) {
+        if (at < want) ids[at] = p + i;
+        ++at;
+      }
+    found += total;
+  }
+  return min(found, want);
+}
+
+// The scratch of the two launches of an append or a compaction (ints in the workspace): per unit [units] each, per page of a unit [units * T]
+struct PgScratch {
+  int32_t *base, *cow, *end;   // append: old length or -1; page to copy from or -1; compaction: 1 if the unit is compacted
+  int32_t *rank, *free_ids, *old;
+};
+
+// Append, first launch: one workgroup.  Item (unit, i) is the i-th page that the unit's new tokens touch.  A page is needed where the
+// table has none, or where others hold it too (then the entries in front of the new ones are copied by the second launch).  Pages go
+// to the items in order, the lowest free one first; a unit whose pages are not all there is left as it is.
+__global__ __launch_bounds__(1024) void k_packed_plan_append(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
+                                                             int32_t* __restrict__ len, int32_t* __restrict__ n_projected, int units,
+                                                             int T, int C, int n_new, PgScratch ws, int32_t* __restrict__ status) {
+  __shared__ int s_wave[16];
+  const int P = min((n_new - 1) / PG_SLOTS + 2, T), tid = threadIdx.x;
+  const long long items = (long long)units * P;
+  int want = 0;
+  for (long long i0 = 0; i0 < items; i0 += 1024) {
+    const long long i = i0 + tid;
+    int need = 0, u = 0;
+    if (i < items) {
+      u = (int)(i / P);
+      const int n = len[u], p = n / PG_SLOTS + (int)(i % P);
+      if (n >= 0 && n <= C - n_new && p <= (n + n_new - 1) / PG_SLOTS) {
+        const int page = table[(size_t)u * T + p];
+        need = !pg_is_page(page, n_pages) || refs[page] > 1;
+      }
+    }
+    int total;
+    const int before = pg_scan(need, s_wave, total);
+    if (i < items) {
+      ws.rank[i] = need ? want + before : -1;
+      if (i % P == P - 1) ws.end[u] = want + before + need;
+    }
+    want += total;
+  }
+  __syncthreads();
+  const int found = want ? pg_find_free(refs, n_pages, want, ws.free_ids, s_wave) : 0;
+  __syncthreads();
+  for (int u = tid; u < units; u += 1024) {
+    const int n = len[u], end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
+    const bool room = n >= 0 && n <= C - n_new, pages = end == begin || end <= found;
+    if (!room) atomicOr(status, IM_STATUS_APPEND_OVERFLOW_BIT);
+    else if (!pages) atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
+    ws.base[u] = room && pages ? n : -1;
+    ws.cow[u] = -1;
+  }
+  __syncthreads();
+  for (long long i = tid; i < items; i += 1024) {
+    const int u = (int)(i / P), n = ws.base[u], r = ws.rank[i];
+    if (n < 0 || r < 0) continue;
+    const int p = n / PG_SLOTS + (int)(i % P), id = ws.free_ids[r];
+    const int old = table[(size_t)u * T + p];
+    table[(size_t)u * T + p] = id;
+    refs[id] = 1;
+    if (pg_is_page(old, n_pages)) {
+      atomicSub(&refs[old], 1);
+      if (i % P == 0 && n % PG_SLOTS) ws.cow[u] = old;
+    }
+  }
+  for (int u = tid; u < units; u += 1024) {
+    const int n = ws.base[u];
+    if (n >= 0) len[u] = n_projected[u] = n + n_new;
+  }
+}
+
+// Append, second launch: grid (tiles of 64 new rows, units), 256 threads.  16 lanes per row, 8 dims each.
+__global__ __launch_bounds__(256) void k_packed_append(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
+                                                       bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos,
+                                                       const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new,
+                                                       const int32_t* __restrict__ pos_new, int n_new, int H_kv, int C,
+                                                       const bf16_t* __restrict__ Uk, const bf16_t* __restrict__ norm_w, float rms_eps,
+                                                       PgScratch ws) {
+  __shared__ ProjectSmem sm;
+  const int unit = blockIdx.y, tid = threadIdx.x, base = ws.base[unit];
+  if (base < 0) return;
+  const int32_t* tab = table + (size_t)unit * T;
+  const int row0 = blockIdx.x * 64, l16 = tid & 15;
+  if (blockIdx.x == 0 && ws.cow[unit] >= 0) {
+    const char* src = pages + (size_t)ws.cow[unit] * PG_BYTES;
+    char* dst = pages + (size_t)tab[base / PG_SLOTS] * PG_BYTES;
+    for (int i = tid; i < base % PG_SLOTS * 34; i += 256) pg_copy_word(src, i / 34, dst, i / 34, i % 34);
+  }
+  for (int row = row0 + (tid >> 4); row < min(row0 + 64, n_new); row += 16) {
+    const size_t at = ((size_t)unit * n_new + row) * IM_D + 8 * l16;
+    const uint4 k = *(const uint4*)(k_new + at), v = *(const uint4*)(v_new + at);
+    const int slot = base + row, r = slot % PG_SLOTS;
+    char* page = pages + (size_t)tab[slot / PG_SLOTS] * PG_BYTES;
+    uint32_t ks, vs;
+    const uint32_t kw = pg_quantise(k, ks), vw = pg_quantise(v, vs);
+    *(uint32_t*)(page + r * 64 + 4 * l16) = kw;
+    *(uint32_t*)(page + pg_v_word(r, l16)) = vw;
+    if (l16 % 4 == 0) {
+      page[PG_KS + 4 * r + l16 / 4] = (char)ks;
+      page[pg_v_scale(r, l16 / 4)] = (char)vs;
+    }
+    if (l16 == 0) pos[(size_t)unit * C + slot] = pos_new[(size_t)(unit / H_kv) * n_new + row];
+  }
+  // indexer keys, from the rows as they were given (row i of k_new is slot base + i of the unit)
+  const bf16_t* K = k_new + ((long long)unit * n_new - ((long long)unit * C + base)) * IM_D;
+  if (n_new <= 4) project_keys_few(K, Kidx, Uk, norm_w, C, rms_eps, unit, base, base + n_new, sm);
+  else if (row0 + 16 * (tid >> 6) < n_new)
+    project_keys_tile(K, Kidx, Uk, norm_w, C, rms_eps, unit, base + row0 + 16 * (tid >> 6), base + n_new, sm);
+}
+
+// Read back: grid (gx, units), 16 lanes per row.  idx NULL: every entry of the unit.
+__global__ __launch_bounds__(256) void k_packed_unpack(const char* __restrict__ pages, int n_pages, const int32_t* __restrict__ table, int T,
+                                                       const int32_t* __restrict__ len, int C, const int32_t* __restrict__ idx,
+                                                       const int32_t* __restrict__ n_idx, bf16_t* __restrict__ K,
+                                                       bf16_t* __restrict__ V, int32_t* __restrict__ status) {
+  const int unit = blockIdx.y, l16 = threadIdx.x & 15, live = min(len[unit], C);
+  const int n = idx ? min(n_idx[unit], C) : live;
+  const int32_t* tab = table + (size_t)unit * T;
+  for (int i = blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += gridDim.x * 16) {
+    const int slot = idx ? idx[(size_t)unit * C + i] : i;
+    if (slot < 0 || slot >= live) continue;
+    const int page_id = tab[slot / PG_SLOTS], r = slot % PG_SLOTS;
+    if (!pg_is_page(page_id, n_pages)) {
+      if (l16 == 0) atomicOr(status, IM_STATUS_BAD_PAGE_BIT);
+      continue;
+    }
+    const char* page = pages + (size_t)page_id * PG_BYTES;
+    const uint32_t kw = *(const uint32_t*)(page + r * 64 + 4 * l16), vw = *(const uint32_t*)(page + pg_v_word(r, l16));
+    const float ks = pg_scale((uint8_t)page[PG_KS + 4 * r + l16 / 4]), vs = pg_scale((uint8_t)page[pg_v_scale(r, l16 / 4)]);
+    const size_t at = ((size_t)unit * C + slot) * IM_D + 8 * l16;
+    *(uint4*)(K + at) = pg_expand(kw, ks);
+    *(uint4*)(V + at) = pg_expand(vw, vs);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// attention of few rows: n_q queries x G heads <= 16 rows per unit
+// ------------------------------------------------------------------------------------------
+struct PgAttn {
+  const char* pages;
+  const int32_t *table, *len, *pos;
+  const bf16_t* q;
+  const int32_t* q_pos;   // NULL: every query sees every entry
+  float* part;            // records [batch][query][head][split]: maximum, denominator, 128 numerators
+  int32_t* status;
+  int n_pages, T, C, H, H_kv, G, n_q, max_live, n_splits;
+  float scale;
+};
+#define PG_REC (IM_D + 2)
+
+// p[tile][r] of 32 keys (head l16, key 16 tile + 4 kq + r) times V; the probabilities go in as two bf16 parts (16 bits: 2^-17 of each,
+// where one part would cost as much as the output's own rounding), o accumulates in fp32
+__device__ __forceinline__ void pg_pv(const float (&p)[2][4], const uint4 (&vf)[2][4], im_c4 (&o)[8]) {
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const im_bf2 a = __builtin_convertvector((im_f2{p[t][2 * h], p[t][2 * h + 1]}), im_bf2);
+      const uint32_t w = __builtin_bit_cast(uint32_t, a);
+      const im_bf2 b = __builtin_convertvector((im_f2{p[t][2 * h] - bf_lo(w), p[t][2 * h + 1] - bf_hi(w)}), im_bf2);
+      hi[2 * t + h] = w;
+      lo[2 * t + h] = __builtin_bit_cast(uint32_t, b);
+    }
+  const im_bf8 ph = __builtin_bit_cast(im_bf8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+  const im_bf8 pl = __builtin_bit_cast(im_bf8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const im_bf8 v = att_column(vf, e);
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, v, o[e], 0, 0, 0);
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, v, o[e], 0, 0, 0);
+  }
+}
+
+// grid (splits, units), 4 waves; a wave takes one page in four of its split: the logits of 64 keys as 4 tiles of 16 x 16 (keys x
+// rows; row r is query r / G, head r % G), the softmax against a running maximum, P V.  The waves' sums meet in LDS.
+template <bool MASK>
+__global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
+  __shared__ float s_ml[4][16][2];
+  __shared__ uint32_t s_nan[4][16];
+  __shared__ __attribute__((aligned(16))) float s_acc[4][16][IM_D];
+  const int unit = blockIdx.y, split = blockIdx.x, b = unit / a.H_kv, h = unit % a.H_kv;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, kq = lane >> 4, l16 = lane & 15;
+  const int n_true = a.len[unit], n = min(n_true, a.max_live), R = a.n_q * a.G;
+  if (n_true > a.max_live && split == 0 && tid == 0) atomicOr(a.status, IM_STATUS_LIVE_EXCEEDED_BIT);
+  const int n_pages = (n + PG_SLOTS - 1) / PG_SLOTS, per = (n_pages + a.n_splits - 1) / a.n_splits;
+  const int p_end = min(n_pages, (split + 1) * per);
+  const int row = min(l16, R - 1), query = row / a.G;
+  const size_t q_row = ((size_t)b * a.n_q + query) * a.H + h * a.G + row % a.G;
+  uint4 qf[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) qf[c] = *(const uint4*)(a.q + q_row * IM_D + 32 * kq + 8 * c);
+  const int q_pos = MASK ? a.q_pos[(size_t)b * a.n_q + query] : 0;
+  const int32_t* tab = a.table + (size_t)unit * a.T;
+  float m = -1e30f, l = 0.f;
+  uint32_t nan_blocks = 0;
+  im_c4 o[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = im_c4{0.f, 0.f, 0.f, 0.f};
+  for (int p = split * per + w; p < p_end; p += 4) {
+    if (!pg_is_page(tab[p], a.n_pages)) {   // a table entry that names no page: nothing is there
+      if (lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
+      continue;
+    }
+    const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
+    const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
+    uint4 kw[4], vw[4];
+    uint32_t ks[4], vs[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      kw[t] = load_stream16(page + t * 1024 + lane / 16 * 16 + l16 * 64);
+      vw[t] = load_stream16(page + PG_V + t * 1024 + lane * 16);
+      ks[t] = (uint8_t)page[PG_KS + 64 * t + 4 * l16 + kq];
+      vs[t] = *(const uint32_t*)(page + PG_VS + 64 * t + 16 * kq + 4 * (l16 >> 2));
+    }
+    float s[4][4], tile_max = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const float f = pg_scale(ks[t]);
+      const uint4 kf[4] = {pg_expand(kw[t].x, f), pg_expand(kw[t].y, f), pg_expand(kw[t].z, f), pg_expand(kw[t].w, f)};
+      const im_c4 acc = att_logits(kf, qf);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = 16 * t + 4 * kq + r;
+        bool seen = key < nk;
+        if (MASK && seen) seen = a.pos[(size_t)unit * a.C + p * PG_SLOTS + key] <= q_pos;
+        s[t][r] = seen ? acc[r] * a.scale : -INFINITY;
+        tile_max = fmaxf(tile_max, s[t][r]);
+      }
+    }
+    tile_max = rows_max_f(tile_max);
+    if (__any(tile_max > m)) {
+      const float m_new = fmaxf(m, tile_max), f = __expf(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {   // the rows of o lie across the lane groups, their factors in lanes 0 .. 15
+        const float fr = __shfl(f, 4 * kq + r, 64);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e][r] *= fr;
+      }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[t][r] = __expf(s[t][r] - m);
+        sum += s[t][r];
+      }
+    l += rows_sum_f(sum);
+    // entries behind the last one hold anything: their values are taken as 0; a block of NaN among the others would reach rows that do
+    // not see it (0 * NaN): it is taken as 0, too, and remembered for the rows that do
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      uint32_t* wv = (uint32_t*)&vw[t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t byte = (vs[t] >> (8 * i)) & 255u;
+        const bool live = 16 * t + 4 * kq + i < nk;
+        if (live && byte == 255u) odd = true;
+        if (!live || byte == 255u) { wv[i] = 0u; vs[t] &= ~(255u << (8 * i)); }
+      }
+    }
+    if (__any(odd)) {
+      for (int key = 0; key < nk; ++key) {
+        uint32_t blocks = 0;
+        for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
+        if (blocks && (!MASK || a.pos[(size_t)unit * a.C + p * PG_SLOTS + key] <= q_pos)) nan_blocks |= blocks;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      uint4 vf[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint4 x = vw[2 * t + u];
+        const uint32_t wv[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vf[u][i] = pg_expand(wv[i], pg_scale((vs[2 * t + u] >> (8 * i)) & 255u));
+      }
+      const float pr[2][4] = {{s[2 * t][0], s[2 * t][1], s[2 * t][2], s[2 * t][3]},
+                              {s[2 * t + 1][0], s[2 * t + 1][1], s[2 * t + 1][2], s[2 * t + 1][3]}};
+      pg_pv(pr, vf, o);
+    }
+  }
+  if (kq == 0) { s_ml[w][l16][0] = m; s_ml[w][l16][1] = l; s_nan[w][l16] = nan_blocks; }
+  att_store(o, &s_acc[w][0][0], l16, kq, min(R, 16));
+  __syncthreads();
+  for (int i = tid; i < R * IM_D; i += 256) {
+    const int r = i >> 7, d = i & 127;
+    const float mm = fmaxf(fmaxf(s_ml[0][r][0], s_ml[1][r][0]), fmaxf(s_ml[2][r][0], s_ml[3][r][0]));
+    float ov = 0.f, lv = 0.f;
+    uint32_t nb = 0;
+#pragma unroll
+    for (int ww = 0; ww < 4; ++ww) {
+      const float f = __expf(s_ml[ww][r][0] - mm);
+      ov = fmaf(f, s_acc[ww][r][d], ov);
+      lv = fmaf(f, s_ml[ww][r][1], lv);
+      nb |= s_nan[ww][r];
+    }
+    if ((nb >> (d >> 5)) & 1u) ov = NAN;
+    const size_t rec_row = ((size_t)b * a.n_q + r / a.G) * a.H + h * a.G + r % a.G;
+    float* rec = a.part + (rec_row * a.n_splits + split) * PG_REC;
+    rec[2 + d] = ov;
+    if (d == 0) { rec[0] = mm; rec[1] = lv; }
+  }
+}
+
+// The splits of a row joined, and the gated memory readout added: grid (batch * n_q * H), 128 threads (thread = output dim).
+__global__ __launch_bounds__(128) void k_packed_combine(const float* __restrict__ part, int n_splits, const bf16_t* __restrict__ q,
+                                                        const bf16_t* __restrict__ Wtheta, const bf16_t* __restrict__ wg, float cg,
+                                                        const float* __restrict__ M, const float* __restrict__ bvec, int H, int H_kv,
+                                                        int n_q, float mem_eps, bf16_t* __restrict__ out,
+                                                        float* __restrict__ readout_dbg) {
+  __shared__ float qs[IM_D], phi[IM_DM], red[2][2];
+  const int tid = threadIdx.x, row = blockIdx.x, j = row % H, b = row / H / n_q;
+  const int unit = b * H_kv + j / (H / H_kv);
+  const float* rec = part + (size_t)row * n_splits * PG_REC;
+  const float qd = bf2f(q[(size_t)row * IM_D + tid]);
+  uint4 wrow[16];
+  const uint4* wr = (const uint4*)(Wtheta + tid * IM_D);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) wrow[i] = wr[i];
+  const float bv = bvec[(size_t)unit * IM_DM + tid], wgv = bf2f(wg[tid]);
+  float mcol[IM_DM];
+  const float* Mu = M + (size_t)unit * IM_DM * IM_D + tid;
+#pragma unroll
+  for (int c = 0; c < IM_DM; ++c) mcol[c] = Mu[c * IM_D];
+  float m = -1e30f, o = 0.f, l = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < n_splits; ++c) m = fmaxf(m, rec[(size_t)c * PG_REC]);
+#pragma unroll 4
+  for (int c = 0; c < n_splits; ++c) {
+    const float f = __expf(rec[(size_t)c * PG_REC] - m);
+    o = fmaf(f, rec[(size_t)c * PG_REC + 2 + tid], o);
+    l = fmaf(f, rec[(size_t)c * PG_REC + 1], l);
+  }
+  const float o_attn = l == 0.f ? 0.f : o / l;   // (no entry seen: 0)
+  qs[tid] = qd;
+  __syncthreads();
+  float ph = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t u[4] = {wrow[i].x, wrow[i].y, wrow[i].z, wrow[i].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ph = fmaf(bf_lo(u[e]), qs[8 * i + 2 * e], ph);
+      ph = fmaf(bf_hi(u[e]), qs[8 * i + 2 * e + 1], ph);
+    }
+  }
+  phi[tid] = ph;
+  float den = wave_sum_f(ph * ph * bv), gz = wave_sum_f(wgv * qd);
+  if ((tid & 63) == 0) { red[tid >> 6][0] = den; red[tid >> 6][1] = gz; }
+  __syncthreads();
+  den = red[0][0] + red[1][0] + mem_eps;
+  gz = red[0][1] + red[1][1] + cg;
+  const float gate = 1.f / (1.f + __expf(-gz));
+  float mr = 0.f;
+#pragma unroll
+  for (int c = 0; c < IM_DM; ++c) mr = fmaf(phi[c], mcol[c], mr);
+  const float res = gate * (mr / den);
+  out[(size_t)row * IM_D + tid] = f2bf_rne(o_attn + res);
+  if (readout_dbg) readout_dbg[(size_t)row * IM_D + tid] = res;
+}
+
+// ------------------------------------------------------------------------------------------
+// attention of many rows
+// ------------------------------------------------------------------------------------------
+#define PG_ROWS 128        // rows of a workgroup: 32 per wave
+#define PG_KP 136          // LDS pitch of a K row (bf16): 16-byte reads of 8 rows fall on all banks
+#define PG_VP 72           // LDS pitch of a dim's 64 values of V
+#define PG_SEG 512         // pages whose masks are looked at together
+
+struct PgReadout {
+  const bf16_t *Wtheta, *wg;
+  const float *M, *b;
+  float cg, mem_eps;
+  bf16_t* out;
+  float* readout_dbg;
+};
+
+__device__ __forceinline__ im_c16 pg_zero16() {
+  im_c16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+__device__ __forceinline__ float halves_max_f(float v) {
+  typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+  const u2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// 8 floats as bf16 operands: nearest, and nearest of what is left
+__device__ __forceinline__ void pg_split8(const float (&x)[8], im_bf8& hi, im_bf8& lo) {
+  uint32_t a[4], r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{x[2 * i], x[2 * i + 1]}), im_bf2));
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{x[2 * i] - bf_lo(a[i]), x[2 * i + 1] - bf_hi(a[i])}), im_bf2));
+  }
+  hi = __builtin_bit_cast(im_bf8, make_uint4(a[0], a[1], a[2], a[3]));
+  lo = __builtin_bit_cast(im_bf8, make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+// grid (row tiles, splits, units), 4 waves; wave w has rows 32 w .. 32 w + 31 of the tile (row r is query r / G, head r % G) as the
+// columns of every product, so that a lane's 16 logits of a block of 32 keys, its running maximum and its sums belong to one row:
+//   S^T = K Q^T, O^T = V^T P^T; products of 32 x 32 x 16, register i of lane (l32, half) is row 8 (i / 4) + 4 half + i % 4, column l32.
+// P^T's registers are its operand as they are; V^T's keys are laid out in LDS in that order (16 t + 8 half + 4 g + j for key
+// 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded to bf16 in LDS by the whole workgroup, the next page's bytes on their way.
+__global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro) {
+  __shared__ __attribute__((aligned(16))) bf16_t s_k[2][PG_SLOTS][PG_KP];
+  __shared__ __attribute__((aligned(16))) bf16_t s_v[2][IM_D][PG_VP];
+  __shared__ __attribute__((aligned(16))) int s_pos[2][PG_SLOTS];
+  __shared__ int s_odd[2][4];
+  __shared__ int s_list[PG_SEG + 1];   // pages to look at; bit 31: some row does not see all of it
+  __shared__ int s_n, s_lim[4][2];
+  const int unit = blockIdx.z, split = blockIdx.y, b = unit / a.H_kv, h = unit % a.H_kv;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+  const int n_true = a.len[unit], n = min(n_true, a.max_live), R = a.n_q * a.G;
+  if (n_true > a.max_live && split == 0 && blockIdx.x == 0 && tid == 0) atomicOr(a.status, IM_STATUS_LIVE_EXCEEDED_BIT);
+  const int n_pages = (n + PG_SLOTS - 1) / PG_SLOTS, per = (n_pages + a.n_splits - 1) / a.n_splits;
+  const int p_begin = split * per, p_end = min(n_pages, p_begin + per);
+  const int my_row = blockIdx.x * PG_ROWS + 32 * w + l32, row = min(my_row, R - 1), query = row / a.G;
+  const size_t q_row = ((size_t)b * a.n_q + query) * a.H + h * a.G + row % a.G;
+  im_bf8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(im_bf8, *(const uint4*)(a.q + q_row * IM_D + 16 * s + 8 * half));
+  const int q_pos = a.q_pos ? a.q_pos[(size_t)b * a.n_q + query] : 0x7fffffff;
+  // the range of the tile's query positions
+  {
+    int lo = q_pos, hi = q_pos;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { lo = min(lo, __shfl_xor(lo, d, 64)); hi = max(hi, __shfl_xor(hi, d, 64)); }
+    if (lane == 0) { s_lim[w][0] = lo; s_lim[w][1] = hi; }
+  }
+  __syncthreads();
+  const int q_lo = min(min(s_lim[0][0], s_lim[1][0]), min(s_lim[2][0], s_lim[3][0]));
+  const int q_hi = max(max(s_lim[0][1], s_lim[1][1]), max(s_lim[2][1], s_lim[3][1]));
+  const int32_t *tab = a.table + (size_t)unit * a.T, *pos = a.pos + (size_t)unit * a.C;
+  const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
+  float m = -1e30f, l = 0.f;
+  uint32_t nan_blocks = 0;
+  im_c16 o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) o[d] = pg_zero16();
+
+  // a thread's share of a page: 32 codes of K (row tid / 4, block tid % 4), and of V (16 keys 16 w .., keys 4 kq .. + 3, dims 8 l16 ..)
+  const int l16 = lane & 15, kq = lane >> 4;
+  uint4 kw, vw;
+  uint32_t ks, vs;
+  int ps = 0;
+  auto fetch = [&](int p) {
+    const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
+    kw = *(const uint4*)(page + 16 * tid);
+    vw = *(const uint4*)(page + PG_V + 16 * tid);
+    ks = (uint8_t)page[PG_KS + tid];
+    vs = *(const uint32_t*)(page + PG_VS + 64 * w + 16 * kq + 4 * (l16 >> 2));
+    if (a.q_pos && tid < PG_SLOTS) ps = p * PG_SLOTS + tid < n ? pos[p * PG_SLOTS + tid] : 0;
+  };
+  auto store = [&](int p, int buf) {
+    const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
+    const float f = pg_scale(ks);
+    uint4* kd = (uint4*)&s_k[buf][tid >> 2][32 * (tid & 3)];
+    kd[0] = pg_expand(kw.x, f);
+    kd[1] = pg_expand(kw.y, f);
+    kd[2] = pg_expand(kw.z, f);
+    kd[3] = pg_expand(kw.w, f);
+    const uint32_t wv[4] = {vw.x, vw.y, vw.z, vw.w};
+    uint4 x[4];
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // (behind the last entry: anything, taken as 0; a block of NaN: see below)
+      const uint32_t byte = (vs >> (8 * i)) & 255u;
+      const bool live = 16 * w + 4 * kq + i < nk;
+      odd |= live && byte == 255u;
+      x[i] = pg_expand(live && byte != 255u ? wv[i] : 0u, pg_scale(live && byte != 255u ? byte : 0u));
+    }
+    if (lane == 0) s_odd[buf][w] = 0;
+    if (__any(odd) && lane == 0) s_odd[buf][w] = 1;
+    bf16_t* vd = &s_v[buf][8 * l16][16 * w + 8 * (kq & 1) + 4 * (kq >> 1)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+      const uint32_t* a0 = (const uint32_t*)&x[0];
+      const uint32_t* a1 = (const uint32_t*)&x[1];
+      const uint32_t* a2 = (const uint32_t*)&x[2];
+      const uint32_t* a3 = (const uint32_t*)&x[3];
+      *(uint2*)(vd + e * PG_VP) = make_uint2(__builtin_amdgcn_perm(a1[e >> 1], a0[e >> 1], sel), __builtin_amdgcn_perm(a3[e >> 1], a2[e >> 1], sel));
+    }
+    if (a.q_pos && tid < PG_SLOTS) s_pos[buf][tid] = ps;
+  };
+
+  for (int seg = p_begin; seg < p_end; seg += PG_SEG) {
+    const int n_seg = min(PG_SEG, p_end - seg);
+    // which pages the tile's rows see, and which of them whole
+    __syncthreads();
+    for (int i = w; i < n_seg; i += 4) {
+      const int first = (seg + i) * PG_SLOTS;
+      int entry = seg + i;
+      if (first + PG_SLOTS > n) entry |= 1 << 31;
+      const bool page = pg_is_page(tab[seg + i], a.n_pages);   // (a table entry that names no page: nothing is there)
+      if (!page && lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
+      if (a.q_pos) {
+        const bool live = first + lane < n;
+        const int at = live ? pos[first + lane] : 0;
+        if (!__any(live && at <= q_hi)) entry = -1;
+        else if (__any(live && at > q_lo)) entry |= 1 << 31;
+      }
+      if (lane == 0) s_list[i] = page ? entry : -1;
+    }
+    __syncthreads();
+    if (w == 0) {   // those that nobody sees leave the list
+      int count = 0;
+      for (int i0 = 0; i0 < n_seg; i0 += 64) {
+        const int entry = i0 + lane < n_seg ? s_list[i0 + lane] : -1;
+        const unsigned long long there = __ballot(entry != -1);
+        if (entry != -1) s_list[count + __popcll(there & ((1ull << lane) - 1ull))] = entry;
+        count += __popcll(there);
+      }
+      if (lane == 0) s_n = count;
+    }
+    __syncthreads();
+    const int count = s_n;
+    if (count == 0) continue;
+    fetch(s_list[0] & 0x7fffffff);
+    store(s_list[0] & 0x7fffffff, 0);
+    __syncthreads();
+    for (int i = 0; i < count; ++i) {
+      const int buf = i & 1, entry = s_list[i], p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
+      const int next = i + 1 < count ? s_list[i + 1] & 0x7fffffff : -1;
+      if (next >= 0) fetch(next);
+      im_c16 sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sc[t] = pg_zero16();
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          const im_bf8 kf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_k[buf][32 * t + l32][16 * s + 8 * half]);
+          sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc[t], 0, 0, 0);
+        }
+      }
+      if (entry < 0) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int key = 32 * t + 8 * g + 4 * half;
+            int4 at = make_int4(0, 0, 0, 0);
+            if (a.q_pos) at = *(const int4*)&s_pos[buf][key];
+            sc[t][4 * g + 0] = key + 0 < nk && at.x <= q_pos ? sc[t][4 * g + 0] : -INFINITY;
+            sc[t][4 * g + 1] = key + 1 < nk && at.y <= q_pos ? sc[t][4 * g + 1] : -INFINITY;
+            sc[t][4 * g + 2] = key + 2 < nk && at.z <= q_pos ? sc[t][4 * g + 2] : -INFINITY;
+            sc[t][4 * g + 3] = key + 3 < nk && at.w <= q_pos ? sc[t][4 * g + 3] : -INFINITY;
+          }
+      }
+      float top = sc[0][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[t][r]);
+      top = halves_max_f(top);
+      if (__any(top > m)) {
+        const float m_new = fmaxf(m, top), f = __builtin_amdgcn_exp2f((m - m_new) * c2);
+        m = m_new;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= f;
+      }
+      const float mc = m * c2;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], c2, -mc));
+          sum += sc[t][r];
+        }
+      l += sum;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {   // 16 keys
+        float pr[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) pr[r] = sc[t >> 1][8 * (t & 1) + r];
+        im_bf8 ph, pl;
+        pg_split8(pr, ph, pl);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const im_bf8 vf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_v[buf][32 * d + l32][16 * t + 8 * half]);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph, o[d], 0, 0, 0);
+        }
+      }
+      if (s_odd[buf][0] | s_odd[buf][1] | s_odd[buf][2] | s_odd[buf][3]) {   // blocks of NaN: for the rows that see them
+        const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
+        for (int key = 0; key < min(nk, PG_SLOTS); ++key) {
+          uint32_t blocks = 0;
+          for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
+          if (blocks && (!a.q_pos || s_pos[buf][key] <= q_pos)) nan_blocks |= blocks;
+        }
+      }
+      if (next >= 0) store(next, buf ^ 1);
+      __syncthreads();
+    }
+  }
+  l = halves_sum_f(l);
+
+  if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_combine
+    if (my_row < R) {
+      float* rec = a.part + (q_row * a.n_splits + split) * PG_REC;
+      if (half == 0) { rec[0] = m * a.scale; rec[1] = l; }
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          rec[2 + 32 * d + 8 * (r >> 2) + 4 * half + (r & 3)] = (nan_blocks >> d) & 1u ? NAN : o[d][r];
+    }
+    return;
+  }
+
+  // the memory readout of the wave's rows: phi^T = Wtheta Q^T, then M^T phi^T with phi and M as two bf16 parts each (2^-16)
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float* Mu = ro.M + (size_t)unit * IM_DM * IM_D;
+  float den = 0.f, gz = 0.f;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const uint4 x = __builtin_bit_cast(uint4, qf[s]), y = *(const uint4*)(ro.wg + 16 * s + 8 * half);
+    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gz = fmaf(bf_lo(xw[e]), bf_lo(yw[e]), fmaf(bf_hi(xw[e]), bf_hi(yw[e]), gz));
+  }
+  im_bf8 ph[8], pl[8];   // operand of 16 values of phi each
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb) {
+    im_c16 phi = pg_zero16();
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const im_bf8 wf = __builtin_bit_cast(im_bf8, *(const uint4*)(ro.Wtheta + (32 * cb + l32) * IM_D + 16 * s + 8 * half));
+      phi = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, qf[s], phi, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) den = fmaf(phi[r] * phi[r], ro.b[(size_t)unit * IM_DM + 32 * cb + 8 * (r >> 2) + 4 * half + (r & 3)], den);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float x[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) x[r] = phi[8 * t + r];
+      pg_split8(x, ph[2 * cb + t], pl[2 * cb + t]);
+    }
+  }
+  den = halves_sum_f(den) + ro.mem_eps;
+  const float gate = 1.f / (1.f + __expf(-(halves_sum_f(gz) + ro.cg))) / den;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    im_c16 mem = pg_zero16();
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {   // 16 of the memory's rows
+      float x[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) x[r] = Mu[(16 * t + 8 * (r >> 2) + 4 * half + (r & 3)) * IM_D + 32 * d + l32];
+      im_bf8 mh, ml;
+      pg_split8(x, mh, ml);
+      mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ml, ph[t], mem, 0, 0, 0);
+      mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mh, pl[t], mem, 0, 0, 0);
+      mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mh, ph[t], mem, 0, 0, 0);
+    }
+    if (my_row < R) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float x[4], res[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          res[r] = gate * mem[4 * g + r];
+          x[r] = ((nan_blocks >> d) & 1u ? NAN : o[d][4 * g + r] * inv) + res[r];
+        }
+        const size_t at = q_row * IM_D + 32 * d + 8 * g + 4 * half;
+        *(uint2*)(ro.out + at) = make_uint2((uint32_t)f2bf_rne(x[0]) | ((uint32_t)f2bf_rne(x[1]) << 16),
+                                            (uint32_t)f2bf_rne(x[2]) | ((uint32_t)f2bf_rne(x[3]) << 16));
+        if (ro.readout_dbg) *(float4*)(ro.readout_dbg + at) = make_float4(res[0], res[1], res[2], res[3]);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// compaction
+// ------------------------------------------------------------------------------------------
+// number of entries of the ascending list [0, n) that are below x
+__device__ __forceinline__ int pg_below(const int32_t* __restrict__ list, int n, int x) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (list[mid] < x) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+// First launch: one workgroup.  A shared page that has a hole below n_keep is copied (a new page is taken for it, in order, as at an
+// append); pages behind n_keep are given up.  The table as it was stays in the scratch for the second launch, which moves the rows.
+__global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
+                                                              const int32_t* __restrict__ len, const int32_t* __restrict__ evict_idx,
+                                                              const int32_t* __restrict__ n_keep, const int32_t* __restrict__ n_evict,
+                                                              int units, int T, int C, int max_live, PgScratch ws,
+                                                              int32_t* __restrict__ status) {
+  __shared__ int s_wave[16];
+  const int tid = threadIdx.x;
+  const long long items = (long long)units * T;
+  int want = 0;
+  for (long long i0 = 0; i0 < items; i0 += 1024) {
+    const long long i = i0 + tid;
+    int need = 0, u = 0;
+    if (i < items) {
+      u = (int)(i / T);
+      const int p = (int)(i % T), nk = n_keep[u], ne = n_evict[u], page = table[i], n = len[u];
+      ws.old[i] = page;
+      if (ne > 0 && nk >= 0 && nk + ne == n && n <= max_live && p * PG_SLOTS < nk && pg_is_page(page, n_pages) && refs[page] > 1) {
+        const int32_t* evict = evict_idx + (size_t)u * C;
+        need = pg_below(evict, ne, p * PG_SLOTS) < pg_below(evict, ne, min(nk, (p + 1) * PG_SLOTS));
+      }
+    }
+    int total;
+    const int before = pg_scan(need, s_wave, total);
+    if (i < items) {
+      ws.rank[i] = need ? want + before : -1;
+      if (i % T == T - 1) ws.end[u] = want + before + need;
+    }
+    want += total;
+  }
+  __syncthreads();
+  const int found = want ? pg_find_free(refs, n_pages, want, ws.free_ids, s_wave) : 0;
+  __syncthreads();
+  for (int u = tid; u < units; u += 1024) {
+    const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
+    const int n = len[u], nk = n_keep[u], ne = n_evict[u];
+    const bool live = n <= max_live, lists = nk >= 0 && ne >= 0 && nk <= n && nk + ne == n, enough = end == begin || end <= found;
+    if (!live) atomicOr(status, IM_STATUS_LIVE_EXCEEDED_BIT);
+    else if (!lists) atomicOr(status, IM_STATUS_BAD_LISTS_BIT);
+    else if (!enough) atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
+    ws.base[u] = live && lists && enough;
+  }
+  __syncthreads();
+  for (long long i = tid; i < items; i += 1024) {
+    const int u = (int)(i / T), p = (int)(i % T), old = ws.old[i], r = ws.rank[i];
+    if (!ws.base[u] || old == -1) continue;
+    if (r >= 0) {
+      const int id = ws.free_ids[r];
+      table[i] = id;
+      refs[id] = 1;
+      atomicSub(&refs[old], 1);
+    } else if (p * PG_SLOTS >= n_keep[u]) {
+      table[i] = -1;
+      if (pg_is_page(old, n_pages)) atomicSub(&refs[old], 1);
+    }
+  }
+}
+
+// Second launch: grid (gx, units), 4 waves; a wave moves an entry, or copies what stays of a page.
+__global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages, int n_pages, const int32_t* __restrict__ table, int T,
+                                                        bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos, int32_t* __restrict__ len,
+                                                        int32_t* __restrict__ n_projected, const int32_t* __restrict__ keep_idx,
+                                                        const int32_t* __restrict__ n_keep, const int32_t* __restrict__ evict_idx,
+                                                        const int32_t* __restrict__ n_evict, int C, PgScratch ws,
+                                                        int32_t* __restrict__ status) {
+  const int unit = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (!ws.base[unit]) return;
+  const int nk = n_keep[unit], ne = n_evict[unit];
+  const int32_t *keep = keep_idx + (size_t)unit * C, *evict = evict_idx + (size_t)unit * C;
+  const int32_t *old = ws.old + (size_t)unit * T, *tab = table + (size_t)unit * T;
+  const int stay = ne < nk ? nk - pg_below(evict, ne, nk) : pg_below(keep, nk, nk);   // kept entries below nk
+  const int moves = nk - stay;
+  for (int j = blockIdx.x * 4 + w; j < moves; j += gridDim.x * 4) {
+    const int ss = keep[stay + j], ds = evict[j];
+    const int ps = (uint32_t)ss < (uint32_t)(nk + ne) ? old[ss / PG_SLOTS] : -1, pd = (uint32_t)ds < (uint32_t)nk ? tab[ds / PG_SLOTS] : -1;
+    if (!pg_is_page(ps, n_pages) || !pg_is_page(pd, n_pages)) {   // a list that names no entry, or a table that names no page
+      if (lane == 0) atomicOr(status, IM_STATUS_BAD_PAGE_BIT);
+      continue;
+    }
+    const char* src = pages + (size_t)ps * PG_BYTES;
+    char* dst = pages + (size_t)pd * PG_BYTES;
+    const size_t is = (size_t)unit * C + ss, id = (size_t)unit * C + ds;
+    if (lane < 34) pg_copy_word(src, ss % PG_SLOTS, dst, ds % PG_SLOTS, lane);
+    else if (lane == 40) pos[id] = pos[is];
+    else if (lane >= 48 && lane < 56) *(uint4*)(Kidx + id * IM_DI + 8 * (lane - 48)) = *(const uint4*)(Kidx + is * IM_DI + 8 * (lane - 48));
+  }
+  if (ne > 0)
+    for (int p = blockIdx.x * 4 + w; p * PG_SLOTS < nk; p += gridDim.x * 4) {
+      if (tab[p] == old[p]) continue;   // (else the first launch has taken a page for it)
+      // the rows of the page that are no holes
+      const int slot = p * PG_SLOTS + lane, at = pg_below(evict, ne, slot);
+      const unsigned long long holes = __ballot(at < ne && evict[at] == slot);
+      const char* src = pages + (size_t)old[p] * PG_BYTES;
+      char* dst = pages + (size_t)tab[p] * PG_BYTES;
+      for (int r = 0; r < min(PG_SLOTS, nk - p * PG_SLOTS); ++r)
+        if (!((holes >> r) & 1ull) && lane < 34) pg_copy_word(src, r, dst, r, lane);
+    }
+  if (blockIdx.x == 0 && threadIdx.x == 0) len[unit] = n_projected[unit] = nk;
+}
+
+// ------------------------------------------------------------------------------------------
+// forks: grid (gx, units), 256 threads
+// ------------------------------------------------------------------------------------------
+// A sequence that stays is only read, one that changes only written, and counts of users only added to or taken from: no order matters.
+__global__ __launch_bounds__(256) void k_packed_fork(const int32_t* __restrict__ src_of, int32_t* __restrict__ table,
+                                                     int32_t* __restrict__ refs, int T, bf16_t* __restrict__ Kidx,
+                                                     int32_t* __restrict__ pos, int32_t* __restrict__ len,
+                                                     int32_t* __restrict__ n_projected, float* __restrict__ M, float* __restrict__ bvec,
+                                                     int n_pages, int B, int H_kv, int C, int32_t* __restrict__ status) {
+  const int unit = blockIdx.y, b = unit / H_kv, from = src_of[b];
+  if (from == b) return;
+  if (from < -1 || from >= B || (from >= 0 && src_of[from] != from)) {
+    if (unit % H_kv == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, IM_STATUS_BAD_FORK_BIT);
+    return;
+  }
+  const int i0 = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * 256;
+  const size_t src = from < 0 ? 0 : (size_t)from * H_kv + unit % H_kv, dst = unit;
+  for (int p = i0; p < T; p += step) {
+    const int had = table[dst * T + p], gets = from < 0 ? -1 : table[src * T + p];
+    if (pg_is_page(gets, n_pages)) atomicAdd(&refs[gets], 1);
+    if (pg_is_page(had, n_pages)) atomicSub(&refs[had], 1);
+    table[dst * T + p] = gets;
+  }
+  const int n = from < 0 ? 0 : min(len[src], C);
+  for (long long i = i0; i < (long long)n * (IM_DI / 8); i += step)
+    ((uint4*)(Kidx + dst * C * IM_DI))[i] = ((const uint4*)(Kidx + src * C * IM_DI))[i];
+  for (int i = i0; i < n; i += step) pos[dst * C + i] = pos[src * C + i];
+  for (int i = i0; i < IM_DM * IM_D / 4; i += step)
+    ((float4*)(M + dst * IM_DM * IM_D))[i] = from < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : ((const float4*)(M + src * IM_DM * IM_D))[i];
+  if (blockIdx.x == 0 && threadIdx.x < IM_DM) bvec[dst * IM_DM + threadIdx.x] = from < 0 ? 0.f : bvec[src * IM_DM + threadIdx.x];
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    len[dst] = from < 0 ? 0 : len[src];
+    n_projected[dst] = from < 0 ? 0 : n_projected[src];
+  }
+}

@@ -16,6 +16,7 @@
 #include "im_score.h"
 #include "im_exact.h"
 #include "im_decode.h"
+#include "im_packed.h"
 
 struct im_handle {
   im_config cfg;
@@ -27,6 +28,7 @@ struct im_handle {
   size_t off_status, off_qy, off_alpha, off_mem, off_attn, off_dpart, off_dml, off_dqm, off_xk, off_dpick, off_darrived, total;
   size_t off_xexp, off_xcount, off_xplanes, off_xlist;              // exact products
   size_t off_spart, off_qf, off_al16, off_qblk, off_recu, off_reci, off_nlist, off_list;   // scores of several queries
+  size_t off_pgunit, off_pgitem, off_pgrec, pg_recs;   // cache in 4 bits: ints per unit, per page of a unit, attention records
   int attn_chunks;
   // optional kernel timing (im_profile_start / im_profile_stop)
   hipEvent_t* prof_ev;
@@ -122,6 +124,9 @@ bool exact_fits(const im_config* c, long long M) {
   return N > 32 && K <= XG_MAX_K && M < (1 << 30) && ((M + 15) / 16) * ((N + 15) / 16) > 2048;
 }
 
+// Records of the many-row attention over packed pages: 34 MB hold those of every launch of up to 512 workgroups
+#define PG_MOST_RECS 65536
+
 size_t n_sets_of(const im_config* c) { return (size_t)c->batch * (c->head_shared ? 1 : c->n_kv_heads); }
 
 // Splits of a set's evicted rows over workgroups (k_mem_partial*), `live` bounding their number: as many as give the 512
@@ -172,7 +177,7 @@ void layout(const im_config* c, im_handle* h) {
   h->off_al16 = take(base, scan ? rows * 16 * sizeof(float) : 0);
   h->off_qblk = take(base, scan ? B * qblk * score_block_bytes(c) : 0);
   h->off_nlist = take(base, scan ? B * sizeof(int32_t) : 0);
-  size_t score = base, mem = base, attn = base, step = base;
+  size_t score = base, mem = base, attn = base, step = base, packed = base;
   // ... the scan's records, listed keys
   const size_t rec_keys = scan ? score_rec_keys(sets, c->capacity) : 0;
   h->off_recu = take(score, rec_keys * 4 * sizeof(float2));
@@ -194,8 +199,19 @@ void layout(const im_config* c, im_handle* h) {
   h->off_xk = take(step, c->head_shared ? B * c->capacity * IM_DI_SHARED * sizeof(double) : 0);
   h->off_dpick = take(step, sets * ((c->capacity + 15) / 16) * sizeof(uint4));
   h->off_darrived = take(step, DEC_LINE * sets * sizeof(int32_t));
+  // the cache in 4 bits (PgScratch; then, in calls of their own, the attention records: one per row and split, pg_splits)
+  const size_t T = (c->capacity + PG_SLOTS - 1) / PG_SLOTS, heads = B * c->n_q_heads;
+  h->off_pgunit = take(packed, 3 * units * sizeof(int32_t));
+  h->off_pgitem = take(packed, 3 * units * T * sizeof(int32_t));
+  size_t queries = h->attn_chunks > 16 ? h->attn_chunks : 16;   // (records per query head)
+  if (c->max_queries > 16) {
+    const size_t many = heads * c->max_queries < PG_MOST_RECS ? c->max_queries : PG_MOST_RECS / heads;
+    if (many > queries) queries = many;
+  }
+  h->pg_recs = c->head_shared ? 0 : heads * queries;
+  h->off_pgrec = take(packed, h->pg_recs * PG_REC * sizeof(float));
   h->total = score;
-  for (size_t end : {mem, attn, step}) h->total = end > h->total ? end : h->total;
+  for (size_t end : {mem, attn, step, packed}) h->total = end > h->total ? end : h->total;
 }
 
 int launch_check(im_handle* h, const char* what) {
@@ -218,6 +234,9 @@ int32_t* status_ptr(im_handle* h) { return (int32_t*)(h->ws + h->off_status); }
 bool state_ok(const im_state* st) {
   return st && st->K && st->V && st->Kidx && st->pos && st->len && st->n_projected && st->M && st->b;
 }
+// a state whose K and V rows are packed pages
+bool dense_ok(const im_state* st) { return st && st->Kidx && st->pos && st->len && st->n_projected && st->M && st->b; }
+bool packed_ok(const im_packed* pk) { return pk && pk->pages && pk->refs && pk->table && pk->n_pages >= 1 && ((uintptr_t)pk->pages & 15) == 0; }
 bool params_ok(const im_params* p) { return p && p->Uq && p->G && p->Uk && p->Wtheta && p->wg; }
 
 // KV heads per set, and the number of sets (what lengths, lists and the memory state are kept per)
@@ -555,7 +574,7 @@ int32_t im_index_score(im_handle* h, const im_params* p, const im_state* st, con
                        void* stream) {
   if (!h) return IM_ERR_INVALID_ARG;
   IM_REQUIRE(params_ok(p), "params has a NULL pointer");
-  IM_REQUIRE(state_ok(st), "state has a NULL pointer");
+  IM_REQUIRE(dense_ok(st), "state has a NULL pointer");
   IM_REQUIRE(q_new && x_gate && q_pos && scores_out, "q_new / x_gate / q_pos / scores_out is NULL");
   IM_REQUIRE(n_q >= 1 && n_q <= h->cfg.max_queries, "n_q must be in 1..max_queries");
   hipStream_t s = (hipStream_t)stream;
@@ -570,13 +589,13 @@ int32_t im_index_score(im_handle* h, const im_params* p, const im_state* st, con
   const double alpha_denom = sqrt((double)(c.n_idx_heads * di));
   if (M <= 32) {
     // a decode-size call: the key projection of the new rows and both query-side products in one launch
-    const int n_proj = c.head_shared ? 0 : units;
+    const int n_proj = c.head_shared || !st->K ? 0 : units;
     k_query_side_few<<<n_proj * IM_PROJ_WGS + (Nq + 1) / 2 + (c.n_idx_heads + 1) / 2, 256, 0, s>>>(
         (const bf16_t*)q_new, (const bf16_t*)p->Uq, qy, Nq, Kq, (const bf16_t*)x_gate, (const bf16_t*)p->G, al,
         c.n_idx_heads, c.gate_in_dim, M, n_proj, (const bf16_t*)st->K, (bf16_t*)st->Kidx, st->len, st->n_projected,
         (const bf16_t*)p->Uk, (const bf16_t*)p->norm_k_w, c.capacity, h->max_live, c.rms_eps, status_ptr(h));
   } else {
-    if (!c.head_shared)
+    if (!c.head_shared && st->K)
       k_project_keys<<<dim3((h->max_live + 63) / 64, units), 256, 0, s>>>(
           (const bf16_t*)st->K, (bf16_t*)st->Kidx, st->len, st->n_projected, (const bf16_t*)p->Uk,
           (const bf16_t*)p->norm_k_w, c.capacity, h->max_live, c.rms_eps, status_ptr(h));
@@ -643,7 +662,7 @@ int32_t im_topb_select(im_handle* h, const float* scores, const im_state* st, in
                        int32_t* keep_idx, int32_t* evict_idx, int32_t* n_keep, int32_t* n_evict,
                        void* stream) {
   if (!h) return IM_ERR_INVALID_ARG;
-  IM_REQUIRE(state_ok(st), "state has a NULL pointer");
+  IM_REQUIRE(dense_ok(st), "state has a NULL pointer");
   IM_REQUIRE(scores && keep_idx && evict_idx && n_keep && n_evict, "an array pointer is NULL");
   IM_REQUIRE(budget >= h->cfg.n_sink + h->cfg.n_recent, "budget is below n_sink + n_recent");
   IM_REQUIRE(budget <= h->cfg.capacity, "budget exceeds capacity");
@@ -963,6 +982,135 @@ int32_t im_decode_step_shared_hidden(im_handle* h, const im_params* p, const im_
   if (!h->cfg.head_shared) return set_err(h, IM_ERR_UNSUPPORTED, "im_decode_step_shared_hidden: head_shared = 0 takes im_decode_step_shared");
   return decode_launch(h, p, st, q, x_new, nullptr, k_new, v_new, pos_new, h->cfg.capacity, lambda, eta, out,
                        readout_dbg, nullptr, nullptr, stream, true, evict_slot, "im_decode_step_shared_hidden");
+}
+
+// ---- the cache held in 4 bits, in pages --------------------------------------------------------------------------
+static PgScratch pg_scratch(im_handle* h) {
+  const size_t units = (size_t)h->cfg.batch * h->cfg.n_kv_heads, T = (h->cfg.capacity + PG_SLOTS - 1) / PG_SLOTS;
+  int32_t *u = (int32_t*)(h->ws + h->off_pgunit), *i = (int32_t*)(h->ws + h->off_pgitem);
+  return {u, u + units, u + 2 * units, i, i + units * T, i + 2 * units * T};
+}
+static int pg_table_pages(const im_config& c) { return (c.capacity + PG_SLOTS - 1) / PG_SLOTS; }
+
+#define IM_REQUIRE_PACKED()                                                                                              \
+  IM_REQUIRE(dense_ok(st), "state has a NULL pointer");                                                                  \
+  IM_REQUIRE(packed_ok(pk), "pages: a NULL pointer, n_pages < 1, or pages not on a 16-byte boundary");                   \
+  if (h->cfg.head_shared) return set_err(h, IM_ERR_UNSUPPORTED, "%s: not built for head_shared = 1", __func__)
+
+int32_t im_append_packed(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* k_new,
+                         const void* v_new, const int32_t* pos_new, int32_t n_new, void* stream) {
+  if (!h) return IM_ERR_INVALID_ARG;
+  IM_REQUIRE(params_ok(p), "params has a NULL pointer");
+  IM_REQUIRE_PACKED();
+  IM_REQUIRE(k_new && v_new && pos_new, "k_new / v_new / pos_new is NULL");
+  IM_REQUIRE(n_new >= 1 && n_new <= h->cfg.capacity, "n_new must be in 1..capacity");
+  hipStream_t s = (hipStream_t)stream;
+  int rc = ensure_ws(h, s);
+  if (rc) return rc;
+  const im_config& c = h->cfg;
+  const int units = c.batch * c.n_kv_heads, T = pg_table_pages(c);
+  const PgScratch ws = pg_scratch(h);
+  k_packed_plan_append<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, st->n_projected, units, T, c.capacity, n_new, ws,
+                                          status_ptr(h));
+  k_packed_append<<<dim3((n_new + 63) / 64, units), 256, 0, s>>>(
+      (char*)pk->pages, pk->table, T, (bf16_t*)st->Kidx, st->pos, (const bf16_t*)k_new, (const bf16_t*)v_new, pos_new, n_new,
+      c.n_kv_heads, c.capacity, (const bf16_t*)p->Uk, (const bf16_t*)p->norm_k_w, c.rms_eps, ws);
+  return launch_check(h, "im_append_packed");
+}
+
+int32_t im_unpack_kv(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* idx, const int32_t* n_idx, void* K_out,
+                     void* V_out, void* stream) {
+  if (!h) return IM_ERR_INVALID_ARG;
+  IM_REQUIRE_PACKED();
+  IM_REQUIRE(K_out && V_out, "K_out / V_out is NULL");
+  IM_REQUIRE((idx && n_idx) || (!idx && !n_idx), "only one of idx / n_idx is NULL");
+  hipStream_t s = (hipStream_t)stream;
+  int rc = ensure_ws(h, s);
+  if (rc) return rc;
+  const im_config& c = h->cfg;
+  const int units = c.batch * c.n_kv_heads;
+  int gx = (c.capacity + 15) / 16;
+  const int most = (4096 + units - 1) / units;
+  if (gx > most) gx = most;
+  k_packed_unpack<<<dim3(gx, units), 256, 0, s>>>((const char*)pk->pages, pk->n_pages, pk->table, pg_table_pages(c), st->len, c.capacity,
+                                                  idx, n_idx, (bf16_t*)K_out, (bf16_t*)V_out, status_ptr(h));
+  return launch_check(h, "im_unpack_kv");
+}
+
+int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* q,
+                                    const int32_t* q_pos, int32_t n_q, void* out, float* readout_dbg, void* stream) {
+  if (!h) return IM_ERR_INVALID_ARG;
+  IM_REQUIRE(params_ok(p), "params has a NULL pointer");
+  IM_REQUIRE_PACKED();
+  IM_REQUIRE(q && out, "q / out is NULL");
+  IM_REQUIRE(n_q >= 1 && (long long)n_q * h->cfg.batch * h->cfg.n_q_heads < (1ll << 31), "n_q must be >= 1, and batch * n_q * n_q_heads below 2^31");
+  hipStream_t s = (hipStream_t)stream;
+  int rc = ensure_ws(h, s);
+  if (rc) return rc;
+  const im_config& c = h->cfg;
+  const int units = c.batch * c.n_kv_heads, G = c.n_q_heads / c.n_kv_heads;
+  const int rows = n_q * G, n_pages = (h->max_live + PG_SLOTS - 1) / PG_SLOTS;
+  const long long all_rows = (long long)c.batch * c.n_q_heads * n_q;
+  const int room = (int)((long long)h->pg_recs / all_rows);   // splits whose records the workspace holds
+  PgAttn a = {};
+  a.pages = (const char*)pk->pages; a.table = pk->table; a.len = st->len; a.pos = st->pos;
+  a.q = (const bf16_t*)q; a.q_pos = q_pos; a.part = (float*)(h->ws + h->off_pgrec); a.status = status_ptr(h);
+  a.n_pages = pk->n_pages; a.T = pg_table_pages(c); a.C = c.capacity; a.H = c.n_q_heads; a.H_kv = c.n_kv_heads; a.G = G; a.n_q = n_q;
+  a.max_live = h->max_live; a.scale = c.softmax_scale;
+  const bool few = rows <= 16;   // (16 records per query head are always there)
+  const int tiles = few ? 1 : (rows + PG_ROWS - 1) / PG_ROWS, wave_pages = few ? 4 : 1;
+  int splits = (int)(((few ? 1024 : 512) + (long long)tiles * units - 1) / ((long long)tiles * units));
+  const int most = (n_pages + wave_pages - 1) / wave_pages;
+  if (splits > most) splits = most;
+  if (splits > room) splits = room;
+  a.n_splits = splits < 1 ? 1 : splits;
+  const bf16_t *Wt = (const bf16_t*)p->Wtheta, *wg = (const bf16_t*)p->wg;
+  if (few) {
+    if (q_pos) k_packed_attn_few<true><<<dim3(a.n_splits, units), 256, 0, s>>>(a);
+    else k_packed_attn_few<false><<<dim3(a.n_splits, units), 256, 0, s>>>(a);
+  } else {
+    const PgReadout ro = {Wt, wg, st->M, st->b, p->cg, c.mem_eps, (bf16_t*)out, readout_dbg};
+    k_packed_attn_many<<<dim3(tiles, a.n_splits, units), 256, 0, s>>>(a, ro);
+  }
+  if (few || a.n_splits > 1)
+    k_packed_combine<<<(unsigned)all_rows, 128, 0, s>>>(a.part, a.n_splits, (const bf16_t*)q, Wt, wg, p->cg, st->M, st->b, c.n_q_heads,
+                                                        c.n_kv_heads, n_q, c.mem_eps, (bf16_t*)out, readout_dbg);
+  return launch_check(h, "im_attn_packed_with_readout");
+}
+
+int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* keep_idx, const int32_t* n_keep,
+                          const int32_t* evict_idx, const int32_t* n_evict, void* stream) {
+  if (!h) return IM_ERR_INVALID_ARG;
+  IM_REQUIRE_PACKED();
+  IM_REQUIRE(keep_idx && n_keep && evict_idx && n_evict, "a list pointer is NULL");
+  hipStream_t s = (hipStream_t)stream;
+  int rc = ensure_ws(h, s);
+  if (rc) return rc;
+  const im_config& c = h->cfg;
+  const int units = c.batch * c.n_kv_heads, T = pg_table_pages(c);
+  const PgScratch ws = pg_scratch(h);
+  k_packed_plan_compact<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity,
+                                           h->max_live, ws, status_ptr(h));
+  int gx = (h->max_live + 3) / 4;
+  if (gx > 64) gx = 64;
+  k_packed_compact<<<dim3(gx, units), 256, 0, s>>>((char*)pk->pages, pk->n_pages, pk->table, T, (bf16_t*)st->Kidx, st->pos, st->len,
+                                                   st->n_projected, keep_idx, n_keep, evict_idx, n_evict, c.capacity, ws, status_ptr(h));
+  return launch_check(h, "im_compact_packed");
+}
+
+int32_t im_fork_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* src_of, void* stream) {
+  if (!h) return IM_ERR_INVALID_ARG;
+  IM_REQUIRE_PACKED();
+  IM_REQUIRE(src_of, "src_of is NULL");
+  hipStream_t s = (hipStream_t)stream;
+  int rc = ensure_ws(h, s);
+  if (rc) return rc;
+  const im_config& c = h->cfg;
+  const int units = c.batch * c.n_kv_heads;
+  k_packed_fork<<<dim3(16, units), 256, 0, s>>>(src_of, pk->table, pk->refs, pg_table_pages(c), (bf16_t*)st->Kidx, st->pos, st->len,
+                                                st->n_projected, st->M, st->b, pk->n_pages, c.batch, c.n_kv_heads, c.capacity,
+                                                status_ptr(h));
+  return launch_check(h, "im_fork_packed");
 }
 
 }  // extern "C"

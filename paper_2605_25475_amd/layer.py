@@ -99,3 +99,50 @@ class Layer:
                          self.out, self.readout if debug else None,
                          self.evicted if (debug or want_evicted) else None, self.scores if debug else None)
         return self.out
+
+
+class PackedLayer:
+    """One attention layer whose cache is held in 4 bits, in pages, and the order of the library calls on it.
+
+    n_pages: pages of its pool.  rows: (K, V) buffers [B, H_kv, C, d_head] (bf16) for evicted rows on their way to the memory; layers
+    that run one after another can share them."""
+
+    def __init__(self, handle: B.Handle, params: B.Params, n_pages: int, rows=None, device="cuda"):
+        cfg = handle.cfg
+        self.h, self.p, self.cfg = handle, params, cfg
+        self.st = B.PackedState(cfg, n_pages, device)
+        S, Cc = cfg.set_shape(), cfg.capacity
+        self.rows = rows or tuple(torch.zeros(S + (Cc, cfg.head_dim), dtype=torch.bfloat16, device=device) for _ in range(2))
+        self.evicted_rows = self.st.with_rows(*self.rows)
+        self.scores = torch.empty(S + (Cc,), dtype=torch.float32, device=device)
+        self.keep_idx = torch.empty(S + (Cc,), dtype=torch.int32, device=device)
+        self.evict_idx = torch.empty(S + (Cc,), dtype=torch.int32, device=device)
+        self.n_keep = torch.zeros(S, dtype=torch.int32, device=device)
+        self.n_evict = torch.zeros(S, dtype=torch.int32, device=device)
+
+    def append(self, k_new, v_new, pos_new):
+        B.im_append_packed(self.h, self.p, self.st, k_new, v_new, pos_new)
+
+    def attend(self, q, out, q_pos=None, readout=None):
+        """Attention + readout of q [B, n_q, H, d_head]: a decode token (q_pos None), draft tokens or a chunk of a prompt."""
+        B.im_attn_packed_with_readout(self.h, self.p, self.st, q, out, q_pos, readout)
+        return out
+
+    def compress(self, q_win, x_gate_win, q_pos_win, budget, lam, eta):
+        """score -> select -> evicted rows -> memory update -> compact."""
+        h, p, st = self.h, self.p, self.st
+        B.im_index_score(h, p, st, q_win, x_gate_win, q_pos_win, self.scores)
+        B.im_topb_select(h, self.scores, st, budget, self.keep_idx, self.evict_idx, self.n_keep, self.n_evict)
+        B.im_unpack_kv(h, st, *self.rows, self.evict_idx, self.n_evict)
+        B.im_memory_update(h, p, self.evicted_rows, self.evict_idx, self.n_evict, lam, eta)
+        B.im_compact_packed(h, st, self.keep_idx, self.n_keep, self.evict_idx, self.n_evict)
+
+    def step(self, k_new, v_new, pos_new, q_new, x_gate, q_pos, q_attn, out, budget, lam, eta, readout=None):
+        """The step of Layer.step on this cache."""
+        self.append(k_new, v_new, pos_new)
+        self.compress(q_new, x_gate, q_pos, budget, lam, eta)
+        return self.attend(q_attn, out, None, readout)
+
+    def fork(self, src_of):
+        """Sequences become copies of others (pages shared), or end: see im_fork_packed."""
+        B.im_fork_packed(self.h, self.st, src_of)
