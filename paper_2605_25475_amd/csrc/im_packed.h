@@ -105,24 +105,18 @@ __device__ __forceinline__ int pg_scan(int v, int* s_wave, int& total) {
 }
 
 // The lowest `want` free pages (refs = 0), ascending, to ids; returns how many there are of them.  One workgroup.
+#define PG_LOOK 16   // pages a thread looks at together
 __device__ __forceinline__ int pg_find_free(const int32_t* __restrict__ refs, int n_pages, int want, int32_t* ids, int* s_wave) {
   int found = 0;
-  for (int p0 = 0; p0 < n_pages && found < want; p0 += 4096) {
-    const int p = p0 + 4 * threadIdx.x;
-    bool f[4];
-    int c = 0, total;
+  for (long long p0 = 0; p0 < n_pages && found < want; p0 += 1024 * PG_LOOK) {
+    const long long p = p0 + PG_LOOK * threadIdx.x;
+    uint32_t f = 0;
+    int total;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = p + i < n_pages && refs[p + i] == 0;
-      c += f[i];
-    }
-    int at = found + pg_scan(c, s_wave, total);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (f[i]) {
-        if (at < want) ids[at] = p + i;
-        ++at;
-      }
+    for (int i = 0; i < PG_LOOK; ++i)
+      if (p + i < n_pages) f |= refs[p + i] == 0 ? 1u << i : 0u;
+    int at = found + pg_scan(__popc(f), s_wave, total);
+    for (; f && at < want; f &= f - 1) ids[at++] = (int)p + __ffs(f) - 1;
     found += total;
   }
   return min(found, want);
@@ -321,22 +315,37 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
   im_c4 o[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = im_c4{0.f, 0.f, 0.f, 0.f};
-  for (int p = split * per + w; p < p_end; p += 4) {
-    if (!pg_is_page(tab[p], a.n_pages)) {   // a table entry that names no page: nothing is there
+  // the next page's bytes are on their way while a page is worked on
+  uint4 kw[4], vw[4], kw_next[4], vw_next[4];
+  uint32_t ks[4], vs[4], ks_next[4], vs_next[4];
+  auto fetch = [&](int p) {   // false: a table entry that names no page: nothing is there
+    const int id = tab[p];
+    if (!pg_is_page(id, a.n_pages)) {
       if (lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
-      continue;
+      return false;
     }
-    const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
-    const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
-    uint4 kw[4], vw[4];
-    uint32_t ks[4], vs[4];
+    const char* page = a.pages + (size_t)id * PG_BYTES;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      kw[t] = load_stream16(page + t * 1024 + lane / 16 * 16 + l16 * 64);
-      vw[t] = load_stream16(page + PG_V + t * 1024 + lane * 16);
-      ks[t] = (uint8_t)page[PG_KS + 64 * t + 4 * l16 + kq];
-      vs[t] = *(const uint32_t*)(page + PG_VS + 64 * t + 16 * kq + 4 * (l16 >> 2));
+      kw_next[t] = load_stream16(page + 1024 * t + 64 * l16 + 16 * kq);
+      ks_next[t] = (uint8_t)page[PG_KS + 64 * t + 4 * l16 + kq];
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      vw_next[t] = load_stream16(page + PG_V + 1024 * t + 16 * lane);
+      vs_next[t] = *(const uint32_t*)(page + PG_VS + 64 * t + 16 * kq + 4 * (l16 >> 2));
+    }
+    return true;
+  };
+  int p = split * per + w;
+  bool there = p < p_end && fetch(p);
+  for (; p < p_end; p += 4) {
+    const bool now = there;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) { kw[t] = kw_next[t]; vw[t] = vw_next[t]; ks[t] = ks_next[t]; vs[t] = vs_next[t]; }
+    there = p + 4 < p_end && fetch(p + 4);
+    if (!now) continue;
+    const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
     float s[4][4], tile_max = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -388,6 +397,7 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
       }
     }
     if (__any(odd)) {
+      const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
       for (int key = 0; key < nk; ++key) {
         uint32_t blocks = 0;
         for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
@@ -432,61 +442,112 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
   }
 }
 
-// The splits of a row joined, and the gated memory readout added: grid (batch * n_q * H), 128 threads (thread = output dim).
-__global__ __launch_bounds__(128) void k_packed_combine(const float* __restrict__ part, int n_splits, const bf16_t* __restrict__ q,
+// The splits of a row joined, and the gated memory readout added: grid (ceil(n_q G / RW), units), 512 threads, RW rows of a unit per
+// workgroup.  Thread (x, g) has column x of the memory in rows 32 g .. 32 g + 31, row x of Wtheta in dims 32 g .. 32 g + 31, and of the
+// splits every fourth: four short chains that meet in LDS, instead of one of 128 steps.
+template <int RW>
+__global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict__ part, int n_splits, const bf16_t* __restrict__ q,
                                                         const bf16_t* __restrict__ Wtheta, const bf16_t* __restrict__ wg, float cg,
                                                         const float* __restrict__ M, const float* __restrict__ bvec, int H, int H_kv,
-                                                        int n_q, float mem_eps, bf16_t* __restrict__ out,
+                                                        int G, int n_q, float mem_eps, bf16_t* __restrict__ out,
                                                         float* __restrict__ readout_dbg) {
-  __shared__ float qs[IM_D], phi[IM_DM], red[2][2];
-  const int tid = threadIdx.x, row = blockIdx.x, j = row % H, b = row / H / n_q;
-  const int unit = b * H_kv + j / (H / H_kv);
-  const float* rec = part + (size_t)row * n_splits * PG_REC;
-  const float qd = bf2f(q[(size_t)row * IM_D + tid]);
-  uint4 wrow[16];
-  const uint4* wr = (const uint4*)(Wtheta + tid * IM_D);
+  __shared__ float s_q[RW][IM_D], s_phi[RW][IM_DM], s_sum[4][RW][IM_D], s_o[4][RW][IM_D], s_ml[4][RW][2], s_red[RW][2][2];
+  const int unit = blockIdx.y, b = unit / H_kv, h = unit % H_kv, tid = threadIdx.x, x = tid & 127, g = tid >> 7;
+  const int r0 = blockIdx.x * RW, R = n_q * G;
+  auto row_of = [&](int i) {   // row i of the workgroup, in [batch][query][head]; rows behind the last repeat it
+    const int r = min(r0 + i, R - 1);
+    return ((size_t)b * n_q + r / G) * H + h * G + r % G;
+  };
+  float mcol[32];
+  const float* Mu = M + ((size_t)unit * IM_DM + 32 * g) * IM_D + x;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) wrow[i] = wr[i];
-  const float bv = bvec[(size_t)unit * IM_DM + tid], wgv = bf2f(wg[tid]);
-  float mcol[IM_DM];
-  const float* Mu = M + (size_t)unit * IM_DM * IM_D + tid;
+  for (int c = 0; c < 32; ++c) mcol[c] = Mu[c * IM_D];
+  uint4 wrow[4];
 #pragma unroll
-  for (int c = 0; c < IM_DM; ++c) mcol[c] = Mu[c * IM_D];
-  float m = -1e30f, o = 0.f, l = 0.f;
-#pragma unroll 4
-  for (int c = 0; c < n_splits; ++c) m = fmaxf(m, rec[(size_t)c * PG_REC]);
-#pragma unroll 4
-  for (int c = 0; c < n_splits; ++c) {
-    const float f = __expf(rec[(size_t)c * PG_REC] - m);
-    o = fmaf(f, rec[(size_t)c * PG_REC + 2 + tid], o);
-    l = fmaf(f, rec[(size_t)c * PG_REC + 1], l);
-  }
-  const float o_attn = l == 0.f ? 0.f : o / l;   // (no entry seen: 0)
-  qs[tid] = qd;
-  __syncthreads();
-  float ph = 0.f;
+  for (int i = 0; i < 4; ++i) wrow[i] = *(const uint4*)(Wtheta + x * IM_D + 32 * g + 8 * i);
+  const float bv = bvec[(size_t)unit * IM_DM + x], wgv = bf2f(wg[x]);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const uint32_t u[4] = {wrow[i].x, wrow[i].y, wrow[i].z, wrow[i].w};
+  for (int i = 0; i < RW; ++i)
+    if (i % 4 == g) s_q[i][x] = bf2f(q[row_of(i) * IM_D + x]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      ph = fmaf(bf_lo(u[e]), qs[8 * i + 2 * e], ph);
-      ph = fmaf(bf_hi(u[e]), qs[8 * i + 2 * e + 1], ph);
+  for (int i = 0; i < RW; ++i) {
+    const float* rec = part + row_of(i) * n_splits * PG_REC;
+    float m = -1e30f, l = 0.f, o = 0.f;
+    for (int c0 = g; c0 < n_splits; c0 += 32) {   // 8 splits at a time
+      float cm[8], cl[8], co[8], top = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float* p = rec + (size_t)min(c0 + 4 * j, n_splits - 1) * PG_REC;
+        cm[j] = p[0]; cl[j] = p[1]; co[j] = p[2 + x];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c0 + 4 * j < n_splits) top = fmaxf(top, cm[j]);
+      const float f = __expf(m - top);
+      l *= f; o *= f; m = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (c0 + 4 * j < n_splits) {
+          const float e = __expf(cm[j] - m);
+          l = fmaf(e, cl[j], l);
+          o = fmaf(e, co[j], o);
+        }
+      }
     }
+    s_o[g][i][x] = o;
+    if (x == 0) { s_ml[g][i][0] = m; s_ml[g][i][1] = l; }
   }
-  phi[tid] = ph;
-  float den = wave_sum_f(ph * ph * bv), gz = wave_sum_f(wgv * qd);
-  if ((tid & 63) == 0) { red[tid >> 6][0] = den; red[tid >> 6][1] = gz; }
   __syncthreads();
-  den = red[0][0] + red[1][0] + mem_eps;
-  gz = red[0][1] + red[1][1] + cg;
-  const float gate = 1.f / (1.f + __expf(-gz));
-  float mr = 0.f;
 #pragma unroll
-  for (int c = 0; c < IM_DM; ++c) mr = fmaf(phi[c], mcol[c], mr);
-  const float res = gate * (mr / den);
-  out[(size_t)row * IM_D + tid] = f2bf_rne(o_attn + res);
-  if (readout_dbg) readout_dbg[(size_t)row * IM_D + tid] = res;
+  for (int i = 0; i < RW; ++i) {
+    float ph = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t u[4] = {wrow[j].x, wrow[j].y, wrow[j].z, wrow[j].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ph = fmaf(bf_lo(u[e]), s_q[i][32 * g + 8 * j + 2 * e], ph);
+        ph = fmaf(bf_hi(u[e]), s_q[i][32 * g + 8 * j + 2 * e + 1], ph);
+      }
+    }
+    s_sum[g][i][x] = ph;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < RW; ++i)
+    if (i % 4 == g) {
+      const float ph = (s_sum[0][i][x] + s_sum[1][i][x]) + (s_sum[2][i][x] + s_sum[3][i][x]);
+      s_phi[i][x] = ph;
+      const float den = wave_sum_f(ph * ph * bv), gz = wave_sum_f(wgv * s_q[i][x]);
+      if ((tid & 63) == 0) { s_red[i][x >> 6][0] = den; s_red[i][x >> 6][1] = gz; }
+    }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    float mr = 0.f;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) mr = fmaf(s_phi[i][32 * g + c], mcol[c], mr);
+    s_sum[g][i][x] = mr;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < RW; ++i)
+    if (i % 4 == g && r0 + i < R) {
+      const float m = fmaxf(fmaxf(s_ml[0][i][0], s_ml[1][i][0]), fmaxf(s_ml[2][i][0], s_ml[3][i][0]));
+      float o = 0.f, l = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = __expf(s_ml[k][i][0] - m);
+        o = fmaf(f, s_o[k][i][x], o);
+        l = fmaf(f, s_ml[k][i][1], l);
+      }
+      const float den = s_red[i][0][0] + s_red[i][1][0] + mem_eps, gz = s_red[i][0][1] + s_red[i][1][1] + cg;
+      const float mr = (s_sum[0][i][x] + s_sum[1][i][x]) + (s_sum[2][i][x] + s_sum[3][i][x]);
+      const float res = 1.f / (1.f + __expf(-gz)) * (mr / den);
+      const size_t at = row_of(i) * IM_D + x;
+      out[at] = f2bf_rne((l == 0.f ? 0.f : o / l) + res);   // (no entry seen: 0)
+      if (readout_dbg) readout_dbg[at] = res;
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -812,63 +873,96 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 // ------------------------------------------------------------------------------------------
 // compaction
 // ------------------------------------------------------------------------------------------
-// number of entries of the ascending list [0, n) that are below x
+// number of entries of the ascending list [0, n) that are below x; for a whole wave: 64 probes a round, 2 rounds for 4096 entries
 __device__ __forceinline__ int pg_below(const int32_t* __restrict__ list, int n, int x) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (list[mid] < x) lo = mid + 1; else hi = mid;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;   // the answer is in [lo, hi]
+  while (hi > lo) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;   // (at is ascending: the lanes whose entry is below x come first)
+    const int c = __popcll(__ballot(at < hi && list[at] < x));
+    if (c == 0) return lo;
+    hi = min(hi, lo + c * step);
+    lo += (c - 1) * step + 1;
   }
   return lo;
 }
 
 // First launch: one workgroup.  A shared page that has a hole below n_keep is copied (a new page is taken for it, in order, as at an
 // append); pages behind n_keep are given up.  The table as it was stays in the scratch for the second launch, which moves the rows.
+#define PG_SHARED (-2)   // ranks before they are numbers: a shared page; one with a hole
+#define PG_HOLE (-3)
 __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
                                                               const int32_t* __restrict__ len, const int32_t* __restrict__ evict_idx,
                                                               const int32_t* __restrict__ n_keep, const int32_t* __restrict__ n_evict,
                                                               int units, int T, int C, int max_live, PgScratch ws,
                                                               int32_t* __restrict__ status) {
-  __shared__ int s_wave[16];
-  const int tid = threadIdx.x;
+  __shared__ int s_wave[16], s_shared;
+  const int tid = threadIdx.x, lane = tid & 63;
   const long long items = (long long)units * T;
-  int want = 0;
-  for (long long i0 = 0; i0 < items; i0 += 1024) {
-    const long long i = i0 + tid;
-    int need = 0, u = 0;
-    if (i < items) {
-      u = (int)(i / T);
-      const int p = (int)(i % T), nk = n_keep[u], ne = n_evict[u], page = table[i], n = len[u];
-      ws.old[i] = page;
-      if (ne > 0 && nk >= 0 && nk + ne == n && n <= max_live && p * PG_SLOTS < nk && pg_is_page(page, n_pages) && refs[page] > 1) {
-        const int32_t* evict = evict_idx + (size_t)u * C;
-        need = pg_below(evict, ne, p * PG_SLOTS) < pg_below(evict, ne, min(nk, (p + 1) * PG_SLOTS));
-      }
-    }
-    int total;
-    const int before = pg_scan(need, s_wave, total);
-    if (i < items) {
-      ws.rank[i] = need ? want + before : -1;
-      if (i % T == T - 1) ws.end[u] = want + before + need;
-    }
-    want += total;
-  }
-  __syncthreads();
-  const int found = want ? pg_find_free(refs, n_pages, want, ws.free_ids, s_wave) : 0;
-  __syncthreads();
+  if (tid == 0) s_shared = 0;
   for (int u = tid; u < units; u += 1024) {
-    const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
     const int n = len[u], nk = n_keep[u], ne = n_evict[u];
-    const bool live = n <= max_live, lists = nk >= 0 && ne >= 0 && nk <= n && nk + ne == n, enough = end == begin || end <= found;
+    const bool live = n <= max_live, lists = nk >= 0 && ne >= 0 && nk <= n && nk + ne == n;
     if (!live) atomicOr(status, IM_STATUS_LIVE_EXCEEDED_BIT);
     else if (!lists) atomicOr(status, IM_STATUS_BAD_LISTS_BIT);
-    else if (!enough) atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
-    ws.base[u] = live && lists && enough;
+    ws.base[u] = live && lists;
+    ws.cow[u] = 0;
   }
   __syncthreads();
   for (long long i = tid; i < items; i += 1024) {
+    const int u = (int)(i / T), p = (int)(i % T), page = table[i];
+    const bool shared = ws.base[u] && n_evict[u] > 0 && p * PG_SLOTS < n_keep[u] && pg_is_page(page, n_pages) && refs[page] > 1;
+    ws.old[i] = page;
+    ws.rank[i] = shared ? PG_SHARED : -1;
+    if (shared) ws.cow[u] = s_shared = 1;
+  }
+  __syncthreads();
+  int found = 0;
+  if (s_shared) {
+    // which of the shared pages have holes
+    for (int u = tid >> 6; u < units; u += 16) {
+      if (!ws.cow[u]) continue;
+      const int32_t* evict = evict_idx + (size_t)u * C;
+      const int nk = n_keep[u], ne = n_evict[u];
+      bool more = true;
+      for (int e0 = 0; e0 < ne && more; e0 += 256) {
+        int e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = e0 + 64 * j + lane < ne ? evict[e0 + 64 * j + lane] : nk;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((uint32_t)e[j] < (uint32_t)nk && ws.rank[(size_t)u * T + e[j] / PG_SLOTS] == PG_SHARED) ws.rank[(size_t)u * T + e[j] / PG_SLOTS] = PG_HOLE;
+        more = !__any(e[3] >= nk);
+      }
+    }
+    __syncthreads();
+    int want = 0;
+    for (long long i0 = 0; i0 < items; i0 += 1024) {
+      const long long i = i0 + tid;
+      const int need = i < items && ws.rank[i] == PG_HOLE;
+      int total;
+      const int before = pg_scan(need, s_wave, total);
+      if (i < items) {
+        ws.rank[i] = need ? want + before : -1;
+        if (i % T == T - 1) ws.end[i / T] = want + before + need;
+      }
+      want += total;
+    }
+    __syncthreads();
+    found = want ? pg_find_free(refs, n_pages, want, ws.free_ids, s_wave) : 0;
+    __syncthreads();
+    for (int u = tid; u < units; u += 1024) {
+      const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
+      if (end != begin && end > found) {
+        atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
+        ws.base[u] = 0;
+      }
+    }
+    __syncthreads();
+  }
+  for (long long i = tid; i < items; i += 1024) {
     const int u = (int)(i / T), p = (int)(i % T), old = ws.old[i], r = ws.rank[i];
-    if (!ws.base[u] || old == -1) continue;
+    if (old == -1 || !ws.base[u]) continue;
     if (r >= 0) {
       const int id = ws.free_ids[r];
       table[i] = id;
@@ -881,46 +975,124 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
   }
 }
 
-// Second launch: grid (gx, units), 4 waves; a wave moves an entry, or copies what stays of a page.
+// Second launch: grid (gx, units), 4 waves.  The first waves move entries, 16 at a time (a row: K 4 lanes of 16 bytes, V 16 words,
+// indexer key 8 lanes); the last ones make the copied pages, each from its own rows and those that move into its holes.
 __global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages, int n_pages, const int32_t* __restrict__ table, int T,
                                                         bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos, int32_t* __restrict__ len,
                                                         int32_t* __restrict__ n_projected, const int32_t* __restrict__ keep_idx,
                                                         const int32_t* __restrict__ n_keep, const int32_t* __restrict__ evict_idx,
                                                         const int32_t* __restrict__ n_evict, int C, PgScratch ws,
                                                         int32_t* __restrict__ status) {
-  const int unit = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int unit = blockIdx.y, lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), waves = gridDim.x * 4;
   if (!ws.base[unit]) return;
   const int nk = n_keep[unit], ne = n_evict[unit];
+  if (blockIdx.x == 0 && threadIdx.x == 0) len[unit] = n_projected[unit] = nk;
+  if (ne == 0) return;
   const int32_t *keep = keep_idx + (size_t)unit * C, *evict = evict_idx + (size_t)unit * C;
   const int32_t *old = ws.old + (size_t)unit * T, *tab = table + (size_t)unit * T;
   const int stay = ne < nk ? nk - pg_below(evict, ne, nk) : pg_below(keep, nk, nk);   // kept entries below nk
   const int moves = nk - stay;
-  for (int j = blockIdx.x * 4 + w; j < moves; j += gridDim.x * 4) {
-    const int ss = keep[stay + j], ds = evict[j];
-    const int ps = (uint32_t)ss < (uint32_t)(nk + ne) ? old[ss / PG_SLOTS] : -1, pd = (uint32_t)ds < (uint32_t)nk ? tab[ds / PG_SLOTS] : -1;
-    if (!pg_is_page(ps, n_pages) || !pg_is_page(pd, n_pages)) {   // a list that names no entry, or a table that names no page
-      if (lane == 0) atomicOr(status, IM_STATUS_BAD_PAGE_BIT);
-      continue;
+  // the page that slot s was in; none for a list's entry that is no slot, or a table's that is no page
+  auto page_of = [&](int s) {
+    const int id = (uint32_t)s < (uint32_t)(nk + ne) ? old[s / PG_SLOTS] : -1;
+    return pg_is_page(id, n_pages) ? id : -1;
+  };
+  auto at_page = [&](int id) { return pages + (size_t)id * PG_BYTES; };
+  for (int j0 = 16 * wave; j0 < moves; j0 += 16 * waves) {
+    // lane = move (of 16): its slots, the pages they are in; ip: the page to write the row to, none where it is made below
+    const bool mine = lane < 16 && j0 + lane < moves;
+    const int ss = mine ? keep[stay + j0 + lane] : -1, ds = mine ? evict[j0 + lane] : -1;
+    int ps = page_of(ss), pd = (uint32_t)ds < (uint32_t)nk ? tab[ds / PG_SLOTS] : -1;
+    if (mine && (ps < 0 || !pg_is_page(pd, n_pages))) {
+      atomicOr(status, IM_STATUS_BAD_PAGE_BIT);
+      ps = pd = -1;
     }
-    const char* src = pages + (size_t)ps * PG_BYTES;
-    char* dst = pages + (size_t)pd * PG_BYTES;
-    const size_t is = (size_t)unit * C + ss, id = (size_t)unit * C + ds;
-    if (lane < 34) pg_copy_word(src, ss % PG_SLOTS, dst, ds % PG_SLOTS, lane);
-    else if (lane == 40) pos[id] = pos[is];
-    else if (lane >= 48 && lane < 56) *(uint4*)(Kidx + id * IM_DI + 8 * (lane - 48)) = *(const uint4*)(Kidx + is * IM_DI + 8 * (lane - 48));
+    const int ip = pd >= 0 && pd == old[ds / PG_SLOTS] ? pd : -1;
+    const size_t row0 = (size_t)unit * C;
+    uint4 k = {}, ki[2] = {};
+    uint32_t v[4] = {}, ks = 0;
+    uint8_t vs = 0;
+    int at = 0;
+    const int rk = lane >> 2, k_ps = __shfl(ps, rk, 64), k_ss = __shfl(ss, rk, 64), k_ip = __shfl(ip, rk, 64), k_ds = __shfl(ds, rk, 64);
+    if (k_ip >= 0) {
+      k = *(const uint4*)(at_page(k_ps) + 64 * (k_ss % PG_SLOTS) + 16 * (lane & 3));
+      vs = (uint8_t)at_page(k_ps)[pg_v_scale(k_ss % PG_SLOTS, lane & 3)];
+    }
+    int v_ps[4], v_ss[4], v_ip[4], v_ds[4], i_ss[2], i_ds[2];
+    bool i_on[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int r = 4 * t + (lane >> 4);
+      v_ps[t] = __shfl(ps, r, 64); v_ss[t] = __shfl(ss, r, 64); v_ip[t] = __shfl(ip, r, 64); v_ds[t] = __shfl(ds, r, 64);
+      if (v_ip[t] >= 0) v[t] = *(const uint32_t*)(at_page(v_ps[t]) + pg_v_word(v_ss[t] % PG_SLOTS, lane & 15));
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = 8 * t + (lane >> 3);
+      i_ss[t] = __shfl(ss, r, 64); i_ds[t] = __shfl(ds, r, 64); i_on[t] = __shfl(pd, r, 64) >= 0;
+      if (i_on[t]) ki[t] = *(const uint4*)(Kidx + (row0 + i_ss[t]) * IM_DI + 8 * (lane & 7));
+    }
+    if (pd >= 0) at = pos[row0 + ss];
+    if (ip >= 0) ks = *(const uint32_t*)(at_page(ps) + PG_KS + 4 * (ss % PG_SLOTS));
+    // (a row that is read here is written by nobody: sources lie at n_keep and above, destinations below)
+    if (k_ip >= 0) {
+      *(uint4*)(at_page(k_ip) + 64 * (k_ds % PG_SLOTS) + 16 * (lane & 3)) = k;
+      at_page(k_ip)[pg_v_scale(k_ds % PG_SLOTS, lane & 3)] = (char)vs;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (v_ip[t] >= 0) *(uint32_t*)(at_page(v_ip[t]) + pg_v_word(v_ds[t] % PG_SLOTS, lane & 15)) = v[t];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (i_on[t]) *(uint4*)(Kidx + (row0 + i_ds[t]) * IM_DI + 8 * (lane & 7)) = ki[t];
+    if (pd >= 0) pos[row0 + ds] = at;
+    if (ip >= 0) *(uint32_t*)(at_page(ip) + PG_KS + 4 * (ds % PG_SLOTS)) = ks;
   }
-  if (ne > 0)
-    for (int p = blockIdx.x * 4 + w; p * PG_SLOTS < nk; p += gridDim.x * 4) {
-      if (tab[p] == old[p]) continue;   // (else the first launch has taken a page for it)
-      // the rows of the page that are no holes
-      const int slot = p * PG_SLOTS + lane, at = pg_below(evict, ne, slot);
-      const unsigned long long holes = __ballot(at < ne && evict[at] == slot);
-      const char* src = pages + (size_t)old[p] * PG_BYTES;
-      char* dst = pages + (size_t)tab[p] * PG_BYTES;
-      for (int r = 0; r < min(PG_SLOTS, nk - p * PG_SLOTS); ++r)
-        if (!((holes >> r) & 1ull) && lane < 34) pg_copy_word(src, r, dst, r, lane);
+  for (int p = waves - 1 - wave; p * PG_SLOTS < nk; p += waves) {
+    if (tab[p] == old[p]) continue;   // (else the first launch has taken a page for it)
+    // lane = row: where it comes from; holes are evict[first ..] one after another
+    const int first = pg_below(evict, ne, p * PG_SLOTS), slot = p * PG_SLOTS + lane;
+    const int e = first + lane < moves ? evict[first + lane] - p * PG_SLOTS : -1;   // a hole's row in this page
+    unsigned long long holes = 0;
+    for (int i = 0; i < 64; ++i) {
+      const int r = __builtin_amdgcn_readlane(e, i);
+      if ((uint32_t)r >= PG_SLOTS) break;
+      holes |= 1ull << r;
     }
-  if (blockIdx.x == 0 && threadIdx.x == 0) len[unit] = n_projected[unit] = nk;
+    int from = slot < nk ? slot : -1;
+    if ((holes >> lane) & 1ull) from = keep[stay + first + __popcll(holes & ((1ull << lane) - 1ull))];
+    const int from_page = page_of(from), from_row = from & (PG_SLOTS - 1);
+    char* dst = at_page(tab[p]);
+    // K: 16 bytes per lane and step, 4 lanes a row; V: words of 4 rows per lane and step
+    uint4 k[4] = {}, v[4] = {};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int r = 16 * t + (lane >> 2), sp = __shfl(from_page, r, 64), sr = __shfl(from_row, r, 64);
+      if (sp >= 0) k[t] = *(const uint4*)(at_page(sp) + 64 * sr + 16 * (lane & 3));
+      uint32_t* vw = (uint32_t*)&v[t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int rv = 16 * t + 4 * (lane >> 4) + i, vp = __shfl(from_page, rv, 64), vr = __shfl(from_row, rv, 64);
+        if (vp >= 0) vw[i] = *(const uint32_t*)(at_page(vp) + pg_v_word(vr, lane & 15));
+      }
+    }
+    uint32_t ks = 0;
+    uint8_t vs[4] = {};
+    if (from_page >= 0) {
+      ks = *(const uint32_t*)(at_page(from_page) + PG_KS + 4 * from_row);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vs[c] = (uint8_t)at_page(from_page)[pg_v_scale(from_row, c)];
+    }
+    // (rows that come from nowhere lie behind the last kept entry: they may hold anything)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      *(uint4*)(dst + 1024 * t + 16 * lane) = k[t];
+      *(uint4*)(dst + PG_V + 1024 * t + 16 * lane) = v[t];
+    }
+    *(uint32_t*)(dst + PG_KS + 4 * lane) = ks;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) dst[pg_v_scale(lane, c)] = (char)vs[c];
+  }
 }
 
 // ------------------------------------------------------------------------------------------

@@ -1059,7 +1059,7 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
   a.max_live = h->max_live; a.scale = c.softmax_scale;
   const bool few = rows <= 16;   // (16 records per query head are always there)
   const int tiles = few ? 1 : (rows + PG_ROWS - 1) / PG_ROWS, wave_pages = few ? 4 : 1;
-  int splits = (int)(((few ? 1024 : 512) + (long long)tiles * units - 1) / ((long long)tiles * units));
+  int splits = (int)((512 + (long long)tiles * units - 1) / ((long long)tiles * units));
   const int most = (n_pages + wave_pages - 1) / wave_pages;
   if (splits > most) splits = most;
   if (splits > room) splits = room;
@@ -1072,9 +1072,15 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
     const PgReadout ro = {Wt, wg, st->M, st->b, p->cg, c.mem_eps, (bf16_t*)out, readout_dbg};
     k_packed_attn_many<<<dim3(tiles, a.n_splits, units), 256, 0, s>>>(a, ro);
   }
-  if (few || a.n_splits > 1)
-    k_packed_combine<<<(unsigned)all_rows, 128, 0, s>>>(a.part, a.n_splits, (const bf16_t*)q, Wt, wg, p->cg, st->M, st->b, c.n_q_heads,
-                                                        c.n_kv_heads, n_q, c.mem_eps, (bf16_t*)out, readout_dbg);
+  if (few || a.n_splits > 1) {
+    auto combine = [&](auto kernel, int rw) {
+      kernel<<<dim3((rows + rw - 1) / rw, units), 512, 0, s>>>(a.part, a.n_splits, (const bf16_t*)q, Wt, wg, p->cg, st->M, st->b, c.n_q_heads,
+                                                               c.n_kv_heads, G, n_q, c.mem_eps, (bf16_t*)out, readout_dbg);
+    };
+    if (all_rows <= 512 || rows == 1) combine(k_packed_combine<1>, 1);
+    else if (all_rows <= 2048 || rows == 2) combine(k_packed_combine<2>, 2);
+    else combine(k_packed_combine<4>, 4);
+  }
   return launch_check(h, "im_attn_packed_with_readout");
 }
 
@@ -1091,7 +1097,8 @@ int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk,
   const PgScratch ws = pg_scratch(h);
   k_packed_plan_compact<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity,
                                            h->max_live, ws, status_ptr(h));
-  int gx = (h->max_live + 3) / 4;
+  // a wave per 16 moved entries, and per copied page
+  int gx = (h->max_live / 16 + T) / 4 + 1;
   if (gx > 64) gx = 64;
   k_packed_compact<<<dim3(gx, units), 256, 0, s>>>((char*)pk->pages, pk->n_pages, pk->table, T, (bf16_t*)st->Kidx, st->pos, st->len,
                                                    st->n_projected, keep_idx, n_keep, evict_idx, n_evict, c.capacity, ws, status_ptr(h));
