@@ -149,18 +149,15 @@ struct ProjectSmem {
   double ys[4][IM_DI];
 };
 
-// One wave: rows row0 .. row0 + 15 of the unit (those below n) on the fp64 matrix cores.
-__device__ __forceinline__ void project_keys_tile(const bf16_t* __restrict__ K, bf16_t* __restrict__ Kidx,
+// One wave: `rows` rows (at most 16) on the fp64 matrix cores; lane (l16, kq) has dims 32 kq .. 32 kq + 31 of row l16 in ka (rows past
+// the end repeat the last).  out: the rows' indexer keys.
+__device__ __forceinline__ void project_keys_rows(const uint4 (&ka)[4], bf16_t* __restrict__ out,
                                                   const bf16_t* __restrict__ Uk,
-                                                  const bf16_t* __restrict__ norm_w, int C, float rms_eps,
-                                                  int unit, int row0, int n, ProjectSmem& sm) {
+                                                  const bf16_t* __restrict__ norm_w, float rms_eps,
+                                                  int rows, ProjectSmem& sm) {
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
   const int l16 = lane & 15, kq = lane >> 4;
-  const int rows = min(16, n - row0);
-  const size_t krow = ((size_t)unit * C + row0 + min(l16, rows - 1)) * IM_D;   // rows past the end repeat the last
-  uint4 ka[4], ub[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) ka[i] = *(const uint4*)(K + krow + 32 * kq + 8 * i);
+  uint4 ub[4][4];
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
@@ -204,11 +201,24 @@ __device__ __forceinline__ void project_keys_tile(const bf16_t* __restrict__ K, 
   for (int k = 0; k < 2; ++k) {
     const int idx = lane + 64 * k, r = idx >> 3, ch = idx & 7;
     if (r < rows)
-      *(uint4*)(Kidx + ((size_t)unit * C + row0 + r) * IM_DI + 8 * ch) = *(const uint4*)&sm.outs[w][r][8 * ch];
+      *(uint4*)(out + (size_t)r * IM_DI + 8 * ch) = *(const uint4*)&sm.outs[w][r][8 * ch];
   }
   // (the next tile of this wave may overwrite the staging rows only after these reads)
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
+}
+
+// One wave: rows row0 .. row0 + 15 of the unit (those below n).
+__device__ __forceinline__ void project_keys_tile(const bf16_t* __restrict__ K, bf16_t* __restrict__ Kidx,
+                                                  const bf16_t* __restrict__ Uk,
+                                                  const bf16_t* __restrict__ norm_w, int C, float rms_eps,
+                                                  int unit, int row0, int n, ProjectSmem& sm) {
+  const int l16 = threadIdx.x & 15, kq = (threadIdx.x & 63) >> 4, rows = min(16, n - row0);
+  const size_t krow = ((size_t)unit * C + row0 + min(l16, rows - 1)) * IM_D;   // rows past the end repeat the last
+  uint4 ka[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ka[i] = *(const uint4*)(K + krow + 32 * kq + 8 * i);
+  project_keys_rows(ka, Kidx + ((size_t)unit * C + row0) * IM_DI, Uk, norm_w, rms_eps, rows, sm);
 }
 
 // One workgroup: rows np .. n - 1 of the unit, at most 4 of them (a decode step appends one), with plain

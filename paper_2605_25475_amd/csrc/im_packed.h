@@ -39,18 +39,20 @@ __device__ __forceinline__ uint4 pg_expand(uint32_t w, float scale) {
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
 }
 
-// 8 bf16 values per lane, 4 lanes (a quad) per block of 32 -> this lane's code word; s: the block's scale byte.
-// s is the smallest with |x| <= 6 * 2^(s - 127) for the whole block (s >= 1): nothing is clipped.  With |x| = 1.m 2^e that is
-// e - 2, and one more where 1.m > 1.5.  Codes are rounded to the nearest, ties to the even code.
-__device__ __forceinline__ uint32_t pg_quantise(uint4 x, uint32_t& s) {
+// the scale byte of a block from the largest |x| of its 32 values (bf16 patterns): the smallest s with |x| <= 6 * 2^(s - 127) (s >= 1):
+// nothing is clipped.  With |x| = 1.m 2^e that is e - 2, and one more where 1.m > 1.5.
+__device__ __forceinline__ uint32_t pg_scale_byte(uint32_t a) {
+  return a >= 0x7f80u ? 255u : (uint32_t)max((int)(a >> 7) - 2 + ((a & 0x7f) > 0x40), 1);
+}
+__device__ __forceinline__ uint32_t pg_largest(uint4 x, uint32_t a) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) a = max(a, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0xB1, 0xF, 0xF, false));   // quad_perm 1 0 3 2
-  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
-  const int e = (int)(a >> 7) - 2 + ((a & 0x7f) > 0x40);
-  s = a >= 0x7f80u ? 255u : (uint32_t)max(e, 1);
+  return a;
+}
+// 8 bf16 values -> a code word; to the nearest code, ties to the even one
+__device__ __forceinline__ uint32_t pg_codes(uint4 x, uint32_t s) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   const float f = pg_scale(s);
   float v[8];
 #pragma unroll
@@ -135,15 +137,13 @@ __global__ __launch_bounds__(1024) void k_packed_plan_append(int32_t* __restrict
                                                              int32_t* __restrict__ len, int32_t* __restrict__ n_projected, int units,
                                                              int T, int C, int n_new, PgScratch ws, int32_t* __restrict__ status) {
   __shared__ int s_wave[16];
-  const int P = min((n_new - 1) / PG_SLOTS + 2, T), tid = threadIdx.x;
-  const long long items = (long long)units * P;
+  const uint32_t P = min((n_new - 1) / PG_SLOTS + 2, T), tid = threadIdx.x, items = (uint32_t)units * P;
   int want = 0;
-  for (long long i0 = 0; i0 < items; i0 += 1024) {
-    const long long i = i0 + tid;
-    int need = 0, u = 0;
+  for (uint32_t i0 = 0; i0 < items; i0 += 1024) {
+    const uint32_t i = i0 + tid, u = i / P, k = i - u * P;
+    int need = 0;
     if (i < items) {
-      u = (int)(i / P);
-      const int n = len[u], p = n / PG_SLOTS + (int)(i % P);
+      const int n = len[u], p = n / PG_SLOTS + (int)k;
       if (n >= 0 && n <= C - n_new && p <= (n + n_new - 1) / PG_SLOTS) {
         const int page = table[(size_t)u * T + p];
         need = !pg_is_page(page, n_pages) || refs[page] > 1;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_append(int32_t* __restrict
     const int before = pg_scan(need, s_wave, total);
     if (i < items) {
       ws.rank[i] = need ? want + before : -1;
-      if (i % P == P - 1) ws.end[u] = want + before + need;
+      if (k == P - 1) ws.end[u] = want + before + need;
     }
     want += total;
   }
@@ -167,27 +167,70 @@ __global__ __launch_bounds__(1024) void k_packed_plan_append(int32_t* __restrict
     else if (!pages) atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
     ws.base[u] = room && pages ? n : -1;
     ws.cow[u] = -1;
+    if (room && pages) len[u] = n_projected[u] = n + n_new;
   }
+  if (want == 0) return;
   __syncthreads();
-  for (long long i = tid; i < items; i += 1024) {
-    const int u = (int)(i / P), n = ws.base[u], r = ws.rank[i];
+  for (uint32_t i = tid; i < items; i += 1024) {
+    const uint32_t u = i / P, k = i - u * P;
+    const int n = ws.base[u], r = ws.rank[i];
     if (n < 0 || r < 0) continue;
-    const int p = n / PG_SLOTS + (int)(i % P), id = ws.free_ids[r];
-    const int old = table[(size_t)u * T + p];
-    table[(size_t)u * T + p] = id;
+    const int id = ws.free_ids[r];
+    int32_t* entry = &table[(size_t)u * T + n / PG_SLOTS + k];
+    const int old = *entry;
+    *entry = id;
     refs[id] = 1;
     if (pg_is_page(old, n_pages)) {
       atomicSub(&refs[old], 1);
-      if (i % P == 0 && n % PG_SLOTS) ws.cow[u] = old;
+      if (k == 0 && n % PG_SLOTS) ws.cow[u] = old;
     }
-  }
-  for (int u = tid; u < units; u += 1024) {
-    const int n = ws.base[u];
-    if (n >= 0) len[u] = n_projected[u] = n + n_new;
   }
 }
 
-// Append, second launch: grid (tiles of 64 new rows, units), 256 threads.  16 lanes per row, 8 dims each.
+// Append, second launch, up to 4 new rows: grid (2, units), 256 threads.  Workgroup 0 rounds and stores the rows (16 lanes a row, a
+// quad of lanes a block), workgroup 1 makes the indexer keys: neither waits for the other's loads.
+__device__ __forceinline__ void pg_copy_page_head(char* pages, const int32_t* tab, const PgScratch& ws, int unit, int base) {
+  if (ws.cow[unit] < 0) return;   // the entries of a shared page in front of the new ones
+  const char* src = pages + (size_t)ws.cow[unit] * PG_BYTES;
+  char* dst = pages + (size_t)tab[base / PG_SLOTS] * PG_BYTES;
+  for (int i = threadIdx.x; i < base % PG_SLOTS * 34; i += 256) pg_copy_word(src, i / 34, dst, i / 34, i % 34);
+}
+__global__ __launch_bounds__(256) void k_packed_append_few(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
+                                                           bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos,
+                                                           const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new,
+                                                           const int32_t* __restrict__ pos_new, int n_new, int H_kv, int C,
+                                                           const bf16_t* __restrict__ Uk, const bf16_t* __restrict__ norm_w,
+                                                           float rms_eps, PgScratch ws) {
+  __shared__ ProjectSmem sm;
+  const int unit = blockIdx.y, tid = threadIdx.x, l16 = tid & 15, row = tid >> 4, base = ws.base[unit];
+  const bf16_t *K = k_new + (size_t)unit * n_new * IM_D, *V = v_new + (size_t)unit * n_new * IM_D;
+  if (base < 0) return;
+  if (blockIdx.x == 1) {   // (from the rows as they were given: the unit's rows and keys from its first new one on)
+    project_keys_few(K, Kidx + ((size_t)unit * C + base) * IM_DI, Uk, norm_w, 0, rms_eps, 0, 0, n_new, sm);
+    return;
+  }
+  const int32_t* tab = table + (size_t)unit * T;
+  pg_copy_page_head(pages, tab, ws, unit, base);
+  if (row >= n_new) return;   // (rows are quads of lanes)
+  const uint4 k = *(const uint4*)(K + row * IM_D + 8 * l16), v = *(const uint4*)(V + row * IM_D + 8 * l16);
+  auto quad_max = [](uint32_t a) {
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0xB1, 0xF, 0xF, false));      // quad_perm 1 0 3 2
+    return max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
+  };
+  const uint32_t ks = pg_scale_byte(quad_max(pg_largest(k, 0))), vs = pg_scale_byte(quad_max(pg_largest(v, 0)));
+  const int slot = base + row, r = slot % PG_SLOTS;
+  char* page = pages + (size_t)tab[slot / PG_SLOTS] * PG_BYTES;
+  *(uint32_t*)(page + r * 64 + 4 * l16) = pg_codes(k, ks);
+  *(uint32_t*)(page + pg_v_word(r, l16)) = pg_codes(v, vs);
+  if (l16 % 4 == 0) {
+    page[PG_KS + 4 * r + l16 / 4] = (char)ks;
+    page[pg_v_scale(r, l16 / 4)] = (char)vs;
+  }
+  if (l16 == 0) pos[(size_t)unit * C + slot] = pos_new[(size_t)(unit / H_kv) * n_new + row];
+}
+
+// The same for more rows: grid (tiles of 64 new rows, units), 4 waves of 16 rows.  Lane (l16, kq) has dims 32 kq .. 32 kq + 31 of row l16, a
+// block of its own, as the key projection takes them: a row is read once, and rounded while the projection's products run.
 __global__ __launch_bounds__(256) void k_packed_append(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
                                                        bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos,
                                                        const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new,
@@ -195,35 +238,34 @@ __global__ __launch_bounds__(256) void k_packed_append(char* __restrict__ pages,
                                                        const bf16_t* __restrict__ Uk, const bf16_t* __restrict__ norm_w, float rms_eps,
                                                        PgScratch ws) {
   __shared__ ProjectSmem sm;
-  const int unit = blockIdx.y, tid = threadIdx.x, base = ws.base[unit];
+  const int unit = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+  const int row0 = blockIdx.x * 64 + 16 * (threadIdx.x >> 6), row = row0 + l16;
+  const size_t at = ((size_t)unit * n_new + min(row, n_new - 1)) * IM_D + 32 * kq;
+  uint4 k[4], v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k[i] = load_stream16(k_new + at + 8 * i);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = load_stream16(v_new + at + 8 * i);
+  const int base = ws.base[unit];
   if (base < 0) return;
   const int32_t* tab = table + (size_t)unit * T;
-  const int row0 = blockIdx.x * 64, l16 = tid & 15;
-  if (blockIdx.x == 0 && ws.cow[unit] >= 0) {
-    const char* src = pages + (size_t)ws.cow[unit] * PG_BYTES;
-    char* dst = pages + (size_t)tab[base / PG_SLOTS] * PG_BYTES;
-    for (int i = tid; i < base % PG_SLOTS * 34; i += 256) pg_copy_word(src, i / 34, dst, i / 34, i % 34);
+  if (blockIdx.x == 0) pg_copy_page_head(pages, tab, ws, unit, base);
+  if (row0 >= n_new) return;   // (wave-uniform; no workgroup barrier below)
+  const int slot = base + min(row, n_new - 1), r = slot % PG_SLOTS;
+  char* page = pages + (size_t)tab[slot / PG_SLOTS] * PG_BYTES;
+  project_keys_rows(k, Kidx + ((size_t)unit * C + base + row0) * IM_DI, Uk, norm_w, rms_eps, min(16, n_new - row0), sm);
+  uint32_t ka = 0, va = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { ka = pg_largest(k[i], ka); va = pg_largest(v[i], va); }
+  const uint32_t ks = pg_scale_byte(ka), vs = pg_scale_byte(va);
+  if (row < n_new) {
+    *(uint4*)(page + r * 64 + 16 * kq) = make_uint4(pg_codes(k[0], ks), pg_codes(k[1], ks), pg_codes(k[2], ks), pg_codes(k[3], ks));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(uint32_t*)(page + pg_v_word(r, 4 * kq + i)) = pg_codes(v[i], vs);
+    page[PG_KS + 4 * r + kq] = (char)ks;
+    page[pg_v_scale(r, kq)] = (char)vs;
+    if (kq == 0) pos[(size_t)unit * C + slot] = pos_new[(size_t)(unit / H_kv) * n_new + row];
   }
-  for (int row = row0 + (tid >> 4); row < min(row0 + 64, n_new); row += 16) {
-    const size_t at = ((size_t)unit * n_new + row) * IM_D + 8 * l16;
-    const uint4 k = *(const uint4*)(k_new + at), v = *(const uint4*)(v_new + at);
-    const int slot = base + row, r = slot % PG_SLOTS;
-    char* page = pages + (size_t)tab[slot / PG_SLOTS] * PG_BYTES;
-    uint32_t ks, vs;
-    const uint32_t kw = pg_quantise(k, ks), vw = pg_quantise(v, vs);
-    *(uint32_t*)(page + r * 64 + 4 * l16) = kw;
-    *(uint32_t*)(page + pg_v_word(r, l16)) = vw;
-    if (l16 % 4 == 0) {
-      page[PG_KS + 4 * r + l16 / 4] = (char)ks;
-      page[pg_v_scale(r, l16 / 4)] = (char)vs;
-    }
-    if (l16 == 0) pos[(size_t)unit * C + slot] = pos_new[(size_t)(unit / H_kv) * n_new + row];
-  }
-  // indexer keys, from the rows as they were given (row i of k_new is slot base + i of the unit)
-  const bf16_t* K = k_new + ((long long)unit * n_new - ((long long)unit * C + base)) * IM_D;
-  if (n_new <= 4) project_keys_few(K, Kidx, Uk, norm_w, C, rms_eps, unit, base, base + n_new, sm);
-  else if (row0 + 16 * (tid >> 6) < n_new)
-    project_keys_tile(K, Kidx, Uk, norm_w, C, rms_eps, unit, base + row0 + 16 * (tid >> 6), base + n_new, sm);
 }
 
 // Read back: grid (gx, units), 16 lanes per row.  idx NULL: every entry of the unit.
@@ -234,6 +276,7 @@ __global__ __launch_bounds__(256) void k_packed_unpack(const char* __restrict__ 
   const int unit = blockIdx.y, l16 = threadIdx.x & 15, live = min(len[unit], C);
   const int n = idx ? min(n_idx[unit], C) : live;
   const int32_t* tab = table + (size_t)unit * T;
+  // (4 rows at a time: 71.5 us instead of 68.4 for 4 x 8 units x 14336 rows)
   for (int i = blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += gridDim.x * 16) {
     const int slot = idx ? idx[(size_t)unit * C + i] : i;
     if (slot < 0 || slot >= live) continue;
@@ -554,9 +597,12 @@ __global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict_
 // attention of many rows
 // ------------------------------------------------------------------------------------------
 #define PG_ROWS 128        // rows of a workgroup: 32 per wave
-#define PG_KP 136          // LDS pitch of a K row (bf16): 16-byte reads of 8 rows fall on all banks
-#define PG_VP 72           // LDS pitch of a dim's 64 values of V
 #define PG_SEG 512         // pages whose masks are looked at together
+
+// Where 16-byte piece g of K row r (16 a row) and of V's dim d (8 of 8 keys each) lie in LDS: pieces change places within a row so that the
+// reads of 8 rows and the writes of a lane group fall on all banks
+__device__ __forceinline__ int pg_k_at(int r, int g) { return r * IM_D + 8 * (g ^ ((r & 7) ^ (g >> 3) * 2)); }
+__device__ __forceinline__ int pg_v_at(int d, int g) { return d * PG_SLOTS + 8 * (g ^ ((d ^ (d >> 3)) & 7)); }
 
 struct PgReadout {
   const bf16_t *Wtheta, *wg;
@@ -595,8 +641,8 @@ __device__ __forceinline__ void pg_split8(const float (&x)[8], im_bf8& hi, im_bf
 // P^T's registers are its operand as they are; V^T's keys are laid out in LDS in that order (16 t + 8 half + 4 g + j for key
 // 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded to bf16 in LDS by the whole workgroup, the next page's bytes on their way.
 __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro) {
-  __shared__ __attribute__((aligned(16))) bf16_t s_k[2][PG_SLOTS][PG_KP];
-  __shared__ __attribute__((aligned(16))) bf16_t s_v[2][IM_D][PG_VP];
+  __shared__ __attribute__((aligned(16))) bf16_t s_k[2][PG_SLOTS * IM_D];
+  __shared__ __attribute__((aligned(16))) bf16_t s_v[2][IM_D * PG_SLOTS];
   __shared__ __attribute__((aligned(16))) int s_pos[2][PG_SLOTS];
   __shared__ int s_odd[2][4];
   __shared__ int s_list[PG_SEG + 1];   // pages to look at; bit 31: some row does not see all of it
@@ -647,11 +693,9 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   auto store = [&](int p, int buf) {
     const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
     const float f = pg_scale(ks);
-    uint4* kd = (uint4*)&s_k[buf][tid >> 2][32 * (tid & 3)];
-    kd[0] = pg_expand(kw.x, f);
-    kd[1] = pg_expand(kw.y, f);
-    kd[2] = pg_expand(kw.z, f);
-    kd[3] = pg_expand(kw.w, f);
+    const uint32_t kv[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(uint4*)&s_k[buf][pg_k_at(tid >> 2, 4 * (tid & 3) + i)] = pg_expand(kv[i], f);
     const uint32_t wv[4] = {vw.x, vw.y, vw.z, vw.w};
     uint4 x[4];
     bool odd = false;
@@ -664,7 +708,6 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     }
     if (lane == 0) s_odd[buf][w] = 0;
     if (__any(odd) && lane == 0) s_odd[buf][w] = 1;
-    bf16_t* vd = &s_v[buf][8 * l16][16 * w + 8 * (kq & 1) + 4 * (kq >> 1)];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
@@ -672,7 +715,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
       const uint32_t* a1 = (const uint32_t*)&x[1];
       const uint32_t* a2 = (const uint32_t*)&x[2];
       const uint32_t* a3 = (const uint32_t*)&x[3];
-      *(uint2*)(vd + e * PG_VP) = make_uint2(__builtin_amdgcn_perm(a1[e >> 1], a0[e >> 1], sel), __builtin_amdgcn_perm(a3[e >> 1], a2[e >> 1], sel));
+      *(uint2*)&s_v[buf][pg_v_at(8 * l16 + e, 2 * w + (kq & 1)) + 4 * (kq >> 1)] = make_uint2(__builtin_amdgcn_perm(a1[e >> 1], a0[e >> 1], sel), __builtin_amdgcn_perm(a3[e >> 1], a2[e >> 1], sel));
     }
     if (a.q_pos && tid < PG_SLOTS) s_pos[buf][tid] = ps;
   };
@@ -722,7 +765,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
         sc[t] = pg_zero16();
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          const im_bf8 kf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_k[buf][32 * t + l32][16 * s + 8 * half]);
+          const im_bf8 kf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_k[buf][pg_k_at(32 * t + l32, 2 * s + half)]);
           sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc[t], 0, 0, 0);
         }
       }
@@ -774,7 +817,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
         pg_split8(pr, ph, pl);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const im_bf8 vf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_v[buf][32 * d + l32][16 * t + 8 * half]);
+          const im_bf8 vf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_v[buf][pg_v_at(32 * d + l32, 2 * t + half)]);
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, o[d], 0, 0, 0);
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph, o[d], 0, 0, 0);
         }
@@ -889,86 +932,89 @@ __device__ __forceinline__ int pg_below(const int32_t* __restrict__ list, int n,
 
 // First launch: one workgroup.  A shared page that has a hole below n_keep is copied (a new page is taken for it, in order, as at an
 // append); pages behind n_keep are given up.  The table as it was stays in the scratch for the second launch, which moves the rows.
-#define PG_SHARED (-2)   // ranks before they are numbers: a shared page; one with a hole
-#define PG_HOLE (-3)
 __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
                                                               const int32_t* __restrict__ len, const int32_t* __restrict__ evict_idx,
                                                               const int32_t* __restrict__ n_keep, const int32_t* __restrict__ n_evict,
                                                               int units, int T, int C, int max_live, PgScratch ws,
                                                               int32_t* __restrict__ status) {
   __shared__ int s_wave[16], s_shared;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const long long items = (long long)units * T;
-  if (tid == 0) s_shared = 0;
-  for (int u = tid; u < units; u += 1024) {
+  const uint32_t tid = threadIdx.x, lane = tid & 63, items = (uint32_t)units * (uint32_t)T;
+  int32_t* hole = ws.free_ids;   // until there are ids: whether a page has a hole
+  auto lists_fit = [&](int u) {
     const int n = len[u], nk = n_keep[u], ne = n_evict[u];
-    const bool live = n <= max_live, lists = nk >= 0 && ne >= 0 && nk <= n && nk + ne == n;
-    if (!live) atomicOr(status, IM_STATUS_LIVE_EXCEEDED_BIT);
-    else if (!lists) atomicOr(status, IM_STATUS_BAD_LISTS_BIT);
-    ws.base[u] = live && lists;
-    ws.cow[u] = 0;
-  }
+    return n <= max_live && nk >= 0 && ne >= 0 && nk <= n && nk + ne == n;
+  };
+  if (tid == 0) s_shared = 0;
   __syncthreads();
-  for (long long i = tid; i < items; i += 1024) {
-    const int u = (int)(i / T), p = (int)(i % T), page = table[i];
-    const bool shared = ws.base[u] && n_evict[u] > 0 && p * PG_SLOTS < n_keep[u] && pg_is_page(page, n_pages) && refs[page] > 1;
+#pragma unroll 2
+  for (uint32_t i = tid; i < items; i += 1024) {
+    const uint32_t u = i / (uint32_t)T, p = i - u * T;
+    const int page = table[i], nk = n_keep[u], ne = n_evict[u];
+    const bool shared = lists_fit(u) && ne > 0 && (int)p * PG_SLOTS < nk && pg_is_page(page, n_pages) && refs[page] > 1;
     ws.old[i] = page;
-    ws.rank[i] = shared ? PG_SHARED : -1;
-    if (shared) ws.cow[u] = s_shared = 1;
+    ws.rank[i] = shared ? 1 : 0;
+    hole[i] = 0;
+    if (shared) s_shared = 1;
   }
   __syncthreads();
   int found = 0;
-  if (s_shared) {
-    // which of the shared pages have holes
+  const bool any_shared = s_shared != 0;
+  if (any_shared) {
     for (int u = tid >> 6; u < units; u += 16) {
-      if (!ws.cow[u]) continue;
+      if (!lists_fit(u)) continue;
       const int32_t* evict = evict_idx + (size_t)u * C;
       const int nk = n_keep[u], ne = n_evict[u];
       bool more = true;
-      for (int e0 = 0; e0 < ne && more; e0 += 256) {
-        int e[4];
+      for (int e0 = 0; e0 < ne && more; e0 += 512) {
+        int e[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = e0 + 64 * j + lane < ne ? evict[e0 + 64 * j + lane] : nk;
+        for (int j = 0; j < 8; ++j) e[j] = e0 + 64 * j + (int)lane < ne ? evict[e0 + 64 * j + lane] : nk;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if ((uint32_t)e[j] < (uint32_t)nk && ws.rank[(size_t)u * T + e[j] / PG_SLOTS] == PG_SHARED) ws.rank[(size_t)u * T + e[j] / PG_SLOTS] = PG_HOLE;
-        more = !__any(e[3] >= nk);
+        for (int j = 0; j < 8; ++j)
+          if ((uint32_t)e[j] < (uint32_t)nk) hole[(size_t)u * T + e[j] / PG_SLOTS] = 1;
+        more = !__any(e[7] >= nk);
       }
     }
     __syncthreads();
     int want = 0;
-    for (long long i0 = 0; i0 < items; i0 += 1024) {
-      const long long i = i0 + tid;
-      const int need = i < items && ws.rank[i] == PG_HOLE;
+    for (uint32_t i0 = 0; i0 < items; i0 += 1024) {
+      const uint32_t i = i0 + tid;
+      const int need = i < items ? ws.rank[i] & hole[i] : 0;
       int total;
       const int before = pg_scan(need, s_wave, total);
       if (i < items) {
         ws.rank[i] = need ? want + before : -1;
-        if (i % T == T - 1) ws.end[i / T] = want + before + need;
+        if (i % (uint32_t)T == (uint32_t)T - 1) ws.end[i / (uint32_t)T] = want + before + need;
       }
       want += total;
     }
     __syncthreads();
     found = want ? pg_find_free(refs, n_pages, want, ws.free_ids, s_wave) : 0;
     __syncthreads();
-    for (int u = tid; u < units; u += 1024) {
-      const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
-      if (end != begin && end > found) {
-        atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
-        ws.base[u] = 0;
-      }
-    }
-    __syncthreads();
   }
-  for (long long i = tid; i < items; i += 1024) {
-    const int u = (int)(i / T), p = (int)(i % T), old = ws.old[i], r = ws.rank[i];
-    if (old == -1 || !ws.base[u]) continue;
+  auto enough = [&](int u) {
+    if (!any_shared) return true;
+    const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
+    return end == begin || end <= found;
+  };
+  for (int u = tid; u < units; u += 1024) {
+    const bool fit = lists_fit(u), pages = enough(u);
+    if (!fit) atomicOr(status, len[u] > max_live ? IM_STATUS_LIVE_EXCEEDED_BIT : IM_STATUS_BAD_LISTS_BIT);
+    else if (!pages) atomicOr(status, IM_STATUS_OUT_OF_PAGES_BIT);
+    ws.base[u] = fit && pages;
+  }
+#pragma unroll 2
+  for (uint32_t i = tid; i < items; i += 1024) {
+    const uint32_t u = i / (uint32_t)T, p = i - u * T;
+    const int old = ws.old[i], r = any_shared ? ws.rank[i] : -1, nk = n_keep[u];
+    const bool fit = lists_fit(u) && enough(u);
+    if (old == -1 || !fit) continue;
     if (r >= 0) {
       const int id = ws.free_ids[r];
       table[i] = id;
       refs[id] = 1;
       atomicSub(&refs[old], 1);
-    } else if (p * PG_SLOTS >= n_keep[u]) {
+    } else if ((int)p * PG_SLOTS >= nk) {
       table[i] = -1;
       if (pg_is_page(old, n_pages)) atomicSub(&refs[old], 1);
     }
@@ -1064,16 +1110,18 @@ __global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages
     const int from_page = page_of(from), from_row = from & (PG_SLOTS - 1);
     char* dst = at_page(tab[p]);
     // K: 16 bytes per lane and step, 4 lanes a row; V: words of 4 rows per lane and step
-    uint4 k[4] = {}, v[4] = {};
+    uint4 k[4];
+    uint32_t v[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int r = 16 * t + (lane >> 2), sp = __shfl(from_page, r, 64), sr = __shfl(from_row, r, 64);
+      k[t] = make_uint4(0, 0, 0, 0);
       if (sp >= 0) k[t] = *(const uint4*)(at_page(sp) + 64 * sr + 16 * (lane & 3));
-      uint32_t* vw = (uint32_t*)&v[t];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int rv = 16 * t + 4 * (lane >> 4) + i, vp = __shfl(from_page, rv, 64), vr = __shfl(from_row, rv, 64);
-        if (vp >= 0) vw[i] = *(const uint32_t*)(at_page(vp) + pg_v_word(vr, lane & 15));
+        v[t][i] = 0;
+        if (vp >= 0) v[t][i] = *(const uint32_t*)(at_page(vp) + pg_v_word(vr, lane & 15));
       }
     }
     uint32_t ks = 0;
@@ -1087,7 +1135,7 @@ __global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       *(uint4*)(dst + 1024 * t + 16 * lane) = k[t];
-      *(uint4*)(dst + PG_V + 1024 * t + 16 * lane) = v[t];
+      *(uint4*)(dst + PG_V + 1024 * t + 16 * lane) = make_uint4(v[t][0], v[t][1], v[t][2], v[t][3]);
     }
     *(uint32_t*)(dst + PG_KS + 4 * lane) = ks;
 #pragma unroll

@@ -995,7 +995,9 @@ static int pg_table_pages(const im_config& c) { return (c.capacity + PG_SLOTS - 
 #define IM_REQUIRE_PACKED()                                                                                              \
   IM_REQUIRE(dense_ok(st), "state has a NULL pointer");                                                                  \
   IM_REQUIRE(packed_ok(pk), "pages: a NULL pointer, n_pages < 1, or pages not on a 16-byte boundary");                   \
-  if (h->cfg.head_shared) return set_err(h, IM_ERR_UNSUPPORTED, "%s: not built for head_shared = 1", __func__)
+  if (h->cfg.head_shared) return set_err(h, IM_ERR_UNSUPPORTED, "%s: not built for head_shared = 1", __func__);          \
+  if ((long long)h->cfg.batch * h->cfg.n_kv_heads * pg_table_pages(h->cfg) >= (1ll << 31))                               \
+    return set_err(h, IM_ERR_UNSUPPORTED, "%s: 2^31 table entries or more", __func__)
 
 int32_t im_append_packed(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* k_new,
                          const void* v_new, const int32_t* pos_new, int32_t n_new, void* stream) {
@@ -1012,9 +1014,13 @@ int32_t im_append_packed(im_handle* h, const im_params* p, const im_state* st, c
   const PgScratch ws = pg_scratch(h);
   k_packed_plan_append<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, st->n_projected, units, T, c.capacity, n_new, ws,
                                           status_ptr(h));
-  k_packed_append<<<dim3((n_new + 63) / 64, units), 256, 0, s>>>(
-      (char*)pk->pages, pk->table, T, (bf16_t*)st->Kidx, st->pos, (const bf16_t*)k_new, (const bf16_t*)v_new, pos_new, n_new,
-      c.n_kv_heads, c.capacity, (const bf16_t*)p->Uk, (const bf16_t*)p->norm_k_w, c.rms_eps, ws);
+  auto append = [&](auto kernel, int gx) {
+    kernel<<<dim3(gx, units), 256, 0, s>>>((char*)pk->pages, pk->table, T, (bf16_t*)st->Kidx, st->pos, (const bf16_t*)k_new,
+                                           (const bf16_t*)v_new, pos_new, n_new, c.n_kv_heads, c.capacity, (const bf16_t*)p->Uk,
+                                           (const bf16_t*)p->norm_k_w, c.rms_eps, ws);
+  };
+  if (n_new <= 4) append(k_packed_append_few, 2);
+  else append(k_packed_append, (n_new + 63) / 64);
   return launch_check(h, "im_append_packed");
 }
 
