@@ -599,11 +599,6 @@ __global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict_
 #define PG_ROWS 128        // rows of a workgroup: 32 per wave
 #define PG_SEG 512         // pages whose masks are looked at together
 
-// Where 16-byte piece g of K row r (16 a row) and of V's dim d (8 of 8 keys each) lie in LDS: pieces change places within a row so that the
-// reads of 8 rows and the writes of a lane group fall on all banks
-__device__ __forceinline__ int pg_k_at(int r, int g) { return r * IM_D + 8 * (g ^ ((r & 7) ^ (g >> 3) * 2)); }
-__device__ __forceinline__ int pg_v_at(int d, int g) { return d * PG_SLOTS + 8 * (g ^ ((d ^ (d >> 3)) & 7)); }
-
 struct PgReadout {
   const bf16_t *Wtheta, *wg;
   const float *M, *b;
@@ -635,18 +630,54 @@ __device__ __forceinline__ void pg_split8(const float (&x)[8], im_bf8& hi, im_bf
   lo = __builtin_bit_cast(im_bf8, make_uint4(r[0], r[1], r[2], r[3]));
 }
 
+typedef _Float16 im_h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 im_h2 __attribute__((ext_vector_type(2)));
+
+// A page expanded in LDS.  16-byte piece g of K's row r (16 pieces) is at 16 (16 r + (g ^ r % 8 ^ 2 (g / 8))), of V's dim d (8 pieces of 8
+// keys) at 16 (8 d + (g ^ (d ^ d / 8) % 8)): the 8 rows of a read and the lane groups of a write fall on all banks, and the addresses of
+// a thread's pieces are one value XOR constants.
+struct PgTile {
+  __attribute__((aligned(16))) char k[PG_SLOTS * IM_D * 2];
+  __attribute__((aligned(16))) char v[PG_SLOTS * IM_D * 2];
+  __attribute__((aligned(16))) int pos[PG_SLOTS];
+  int odd[4];   // whether the wave's 16 keys hold a block of NaN
+};
+
+// 4 keys x 8 dims of V (a word of codes and a scale byte per key) -> 8 pieces of 4 keys, fp16 values in units of 2^(e - 127).  Scales of
+// e - 22 .. e are taken (exact: a code is at least 0.5), others as 0.
+#define PG_BAND 23
+#define PG_BANDS 5
+__device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, int e, uint2 (&piece)[8]) {
+  const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w};
+  uint32_t x[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int byte = (vs >> (8 * i)) & 255u;
+    const float f = (uint32_t)(e - byte) < PG_BAND ? pg_scale(byte + 127 - e) : 0.f;
+    x[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 0));
+    x[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 1));
+    x[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 2));
+    x[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 3));
+  }
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    const uint32_t sel = (d & 1) ? 0x07060302u : 0x05040100u;
+    piece[d] = make_uint2(__builtin_amdgcn_perm(x[1][d >> 1], x[0][d >> 1], sel), __builtin_amdgcn_perm(x[3][d >> 1], x[2][d >> 1], sel));
+  }
+}
+
 // grid (row tiles, splits, units), 4 waves; wave w has rows 32 w .. 32 w + 31 of the tile (row r is query r / G, head r % G) as the
 // columns of every product, so that a lane's 16 logits of a block of 32 keys, its running maximum and its sums belong to one row:
 //   S^T = K Q^T, O^T = V^T P^T; products of 32 x 32 x 16, register i of lane (l32, half) is row 8 (i / 4) + 4 half + i % 4, column l32.
 // P^T's registers are its operand as they are; V^T's keys are laid out in LDS in that order (16 t + 8 half + 4 g + j for key
-// 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded to bf16 in LDS by the whole workgroup, the next page's bytes on their way.
+// 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded in LDS by the whole workgroup, the next page's bytes on their way.
+//   K goes in as bf16 (exact).  P goes in as fp16, half a step of 2^-11 off each (the sums of P stay fp32), with V as fp16 multiples of 2^e per
+// 32 dims, e the largest scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment
+// is gone over again for the scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
 __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro) {
-  __shared__ __attribute__((aligned(16))) bf16_t s_k[2][PG_SLOTS * IM_D];
-  __shared__ __attribute__((aligned(16))) bf16_t s_v[2][IM_D * PG_SLOTS];
-  __shared__ __attribute__((aligned(16))) int s_pos[2][PG_SLOTS];
-  __shared__ int s_odd[2][4];
-  __shared__ int s_list[PG_SEG + 1];   // pages to look at; bit 31: some row does not see all of it
-  __shared__ int s_n, s_lim[4][2];
+  __shared__ PgTile s_tile[2];
+  __shared__ int s_list[PG_SEG];   // pages to look at; bit 31: some row does not see all of it
+  __shared__ int s_n, s_lim[4][2], s_scale[4][4][2];
   const int unit = blockIdx.z, split = blockIdx.y, b = unit / a.H_kv, h = unit % a.H_kv;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
   const int n_true = a.len[unit], n = min(n_true, a.max_live), R = a.n_q * a.G;
@@ -673,12 +704,16 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
   float m = -1e30f, l = 0.f;
   uint32_t nan_blocks = 0;
+  int e_was[4] = {127, 127, 127, 127};   // o[d] counts in 2^(e_was[d] - 127)
   im_c16 o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] = pg_zero16();
 
-  // a thread's share of a page: 32 codes of K (row tid / 4, block tid % 4), and of V (16 keys 16 w .., keys 4 kq .. + 3, dims 8 l16 ..)
+  // a thread's share of a page: 32 codes of K (row tid / 4, block tid % 4), and of V (keys 16 w + 4 kq .. + 3, dims 8 l16 ..)
   const int l16 = lane & 15, kq = lane >> 4;
+  const int k_put = 256 * (tid >> 2) + 16 * ((4 * (tid & 3)) ^ ((tid >> 2) & 7) ^ ((tid & 2) ? 2 : 0));
+  const int v_put = 1024 * l16 + 16 * ((2 * w + (kq & 1)) ^ (l16 & 7)) + 8 * (kq >> 1);
+  const int k_get = 256 * l32 + 16 * (half ^ (l32 & 7)), v_get = 128 * l32 + 16 * (half ^ (l32 & 7) ^ (l32 >> 3));
   uint4 kw, vw;
   uint32_t ks, vs;
   int ps = 0;
@@ -690,54 +725,170 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     vs = *(const uint32_t*)(page + PG_VS + 64 * w + 16 * kq + 4 * (l16 >> 2));
     if (a.q_pos && tid < PG_SLOTS) ps = p * PG_SLOTS + tid < n ? pos[p * PG_SLOTS + tid] : 0;
   };
-  auto store = [&](int p, int buf) {
-    const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
-    const float f = pg_scale(ks);
-    const uint32_t kv[4] = {kw.x, kw.y, kw.z, kw.w};
+
+  // the listed pages; my_e: the units of this thread's share of V; counted: whether P counts towards the sums
+  auto segment = [&](int count, int my_e, bool counted) {
+    auto store = [&](int p, PgTile& t) {
+      const int nk = n - p * PG_SLOTS;
+      const float f = pg_scale(ks);
+      const uint32_t kv[4] = {kw.x, kw.y, kw.z, kw.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *(uint4*)&s_k[buf][pg_k_at(tid >> 2, 4 * (tid & 3) + i)] = pg_expand(kv[i], f);
-    const uint32_t wv[4] = {vw.x, vw.y, vw.z, vw.w};
-    uint4 x[4];
-    bool odd = false;
+      for (int i = 0; i < 4; ++i) *(uint4*)(t.k + (k_put ^ (16 * i))) = pg_expand(kv[i], f);
+      // entries behind the last one hold anything: taken as 0, as a block of NaN is, which the rows that see it get below
+      bool odd = false;
+      uint4 x = vw;
+      uint32_t sc = vs, y = ~vs;
+      const bool has_255 = ((y - 0x01010101u) & ~y & 0x80808080u) != 0;   // some byte of vs is 255
+      if (__any(has_255 || nk < PG_SLOTS)) {
+        uint32_t xw[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // (behind the last entry: anything, taken as 0; a block of NaN: see below)
-      const uint32_t byte = (vs >> (8 * i)) & 255u;
-      const bool live = 16 * w + 4 * kq + i < nk;
-      odd |= live && byte == 255u;
-      x[i] = pg_expand(live && byte != 255u ? wv[i] : 0u, pg_scale(live && byte != 255u ? byte : 0u));
+        for (int i = 0; i < 4; ++i) {
+          const bool live = 16 * w + 4 * kq + i < nk, nan = ((vs >> (8 * i)) & 255u) == 255u;
+          odd |= live && nan;
+          if (!live || nan) { xw[i] = 0u; sc &= ~(255u << (8 * i)); }
+        }
+        x = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+      }
+      const bool any_odd = __any(odd);
+      if (lane == 0) t.odd[w] = any_odd;
+      uint2 piece[8];
+      pg_v_pieces(x, sc, my_e, piece);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *(uint2*)(t.v + (v_put ^ (16 * e)) + 128 * e) = piece[e];
+      if (a.q_pos && tid < PG_SLOTS) t.pos[tid] = ps;
+    };
+    fetch(s_list[0] & 0x7fffffff);
+    store(s_list[0] & 0x7fffffff, s_tile[0]);
+    __syncthreads();
+    for (int i = 0; i < count; ++i) {
+      const PgTile& t = s_tile[i & 1];
+      const int entry = s_list[i], p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
+      const int next = i + 1 < count ? s_list[i + 1] & 0x7fffffff : -1;
+      if (next >= 0) fetch(next);
+      im_c16 sc[2];
+      sc[0] = pg_zero16();
+      sc[1] = pg_zero16();
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const char* at = t.k + (k_get ^ (16 * ((2 * s) ^ (s >= 4 ? 2 : 0))));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(im_bf8, *(const uint4*)(at + 8192 * u)), qf[s], sc[u], 0, 0, 0);
+      }
+      if (entry < 0) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int key = 32 * u + 8 * g + 4 * half;
+            int4 at = make_int4(0, 0, 0, 0);
+            if (a.q_pos) at = *(const int4*)&t.pos[key];
+            sc[u][4 * g + 0] = key + 0 < nk && at.x <= q_pos ? sc[u][4 * g + 0] : -INFINITY;
+            sc[u][4 * g + 1] = key + 1 < nk && at.y <= q_pos ? sc[u][4 * g + 1] : -INFINITY;
+            sc[u][4 * g + 2] = key + 2 < nk && at.z <= q_pos ? sc[u][4 * g + 2] : -INFINITY;
+            sc[u][4 * g + 3] = key + 3 < nk && at.w <= q_pos ? sc[u][4 * g + 3] : -INFINITY;
+          }
+      }
+      float top = sc[0][0];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[u][r]);
+      top = halves_max_f(top);
+      if (__any(top > m)) {
+        const float m_new = fmaxf(m, top), f = __builtin_amdgcn_exp2f((m - m_new) * c2);
+        m = m_new;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= f;
+      }
+      const float mc = m * c2;
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[u][r] = __builtin_amdgcn_exp2f(fmaf(sc[u][r], c2, -mc));
+          sum[u] += sc[u][r];
+        }
+      l += counted ? sum[0] + sum[1] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {   // 16 keys
+        float pr[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) pr[r] = sc[u >> 1][8 * (u & 1) + r];
+        uint32_t x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{pr[2 * r], pr[2 * r + 1]}), im_h2));
+        const im_h8 pf = __builtin_bit_cast(im_h8, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(im_h8, *(const uint4*)(t.v + 4096 * d + (v_get ^ (16 * ((2 * u) ^ (d & 1 ? 4 : 0)))))), pf, o[d], 0, 0, 0);
+      }
+      if (t.odd[0] | t.odd[1] | t.odd[2] | t.odd[3]) {   // blocks of NaN: for the rows that see them
+        const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
+        for (int key = 0; key < min(nk, PG_SLOTS); ++key) {
+          uint32_t blocks = 0;
+          for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
+          if (blocks && (!a.q_pos || t.pos[key] <= q_pos)) nan_blocks |= blocks;
+        }
+      }
+      if (next >= 0) store(next, s_tile[(i & 1) ^ 1]);
+      __syncthreads();
     }
-    if (lane == 0) s_odd[buf][w] = 0;
-    if (__any(odd) && lane == 0) s_odd[buf][w] = 1;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-      const uint32_t* a0 = (const uint32_t*)&x[0];
-      const uint32_t* a1 = (const uint32_t*)&x[1];
-      const uint32_t* a2 = (const uint32_t*)&x[2];
-      const uint32_t* a3 = (const uint32_t*)&x[3];
-      *(uint2*)&s_v[buf][pg_v_at(8 * l16 + e, 2 * w + (kq & 1)) + 4 * (kq >> 1)] = make_uint2(__builtin_amdgcn_perm(a1[e >> 1], a0[e >> 1], sel), __builtin_amdgcn_perm(a3[e >> 1], a2[e >> 1], sel));
-    }
-    if (a.q_pos && tid < PG_SLOTS) s_pos[buf][tid] = ps;
   };
 
   for (int seg = p_begin; seg < p_end; seg += PG_SEG) {
     const int n_seg = min(PG_SEG, p_end - seg);
-    // which pages the tile's rows see, and which of them whole
+    // which pages the tile's rows see, which of them whole, and the largest and smallest scale (above 1, which is as good as 0) of their
+    // values per block: lane (key / 4, block) looks at 4 keys; 4 pages of a wave at a time
+    int s_hi = 0, s_lo = 255;
     __syncthreads();
-    for (int i = w; i < n_seg; i += 4) {
-      const int first = (seg + i) * PG_SLOTS;
-      int entry = seg + i;
-      if (first + PG_SLOTS > n) entry |= 1 << 31;
-      const bool page = pg_is_page(tab[seg + i], a.n_pages);   // (a table entry that names no page: nothing is there)
-      if (!page && lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
-      if (a.q_pos) {
-        const bool live = first + lane < n;
-        const int at = live ? pos[first + lane] : 0;
-        if (!__any(live && at <= q_hi)) entry = -1;
-        else if (__any(live && at > q_lo)) entry |= 1 << 31;
+    for (int i0 = 4 * w; i0 < n_seg; i0 += 16) {
+      int id[4], at[4];
+      uint32_t sv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int p = seg + min(i0 + j, n_seg - 1);
+        id[j] = tab[p];
+        at[j] = a.q_pos ? pos[min(p * PG_SLOTS + lane, n - 1)] : 0;
       }
-      if (lane == 0) s_list[i] = page ? entry : -1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (!pg_is_page(id[j], a.n_pages)) {   // (a table entry that names no page: nothing is there)
+          if (lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
+          id[j] = -1;
+        }
+        sv[j] = *(const uint32_t*)(a.pages + (size_t)max(id[j], 0) * PG_BYTES + PG_VS + 4 * lane);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + j, first = (seg + i) * PG_SLOTS;
+        if (i >= n_seg) break;
+        int entry = seg + i;
+        if (first + PG_SLOTS > n) entry |= 1 << 31;
+        if (a.q_pos) {
+          const bool live = first + lane < n;
+          if (!__any(live && at[j] <= q_hi)) entry = -1;
+          else if (__any(live && at[j] > q_lo)) entry |= 1 << 31;
+        }
+        if (id[j] < 0) entry = -1;
+        if (lane == 0) s_list[i] = entry;
+        if (entry == -1) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int byte = (sv[j] >> (8 * k)) & 255u;
+          const bool counts = byte != 255 && byte > 1 && first + 4 * (lane >> 2) + k < n;
+          s_hi = counts ? max(s_hi, byte) : s_hi;
+          s_lo = counts ? min(s_lo, byte) : s_lo;
+        }
+      }
     }
+#pragma unroll
+    for (int d = 4; d < 64; d <<= 1) { s_hi = max(s_hi, __shfl_xor(s_hi, d, 64)); s_lo = min(s_lo, __shfl_xor(s_lo, d, 64)); }
+    if (lane < 4) { s_scale[w][lane][0] = s_hi; s_scale[w][lane][1] = s_lo; }
     __syncthreads();
     if (w == 0) {   // those that nobody sees leave the list
       int count = 0;
@@ -752,88 +903,30 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     __syncthreads();
     const int count = s_n;
     if (count == 0) continue;
-    fetch(s_list[0] & 0x7fffffff);
-    store(s_list[0] & 0x7fffffff, 0);
-    __syncthreads();
-    for (int i = 0; i < count; ++i) {
-      const int buf = i & 1, entry = s_list[i], p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
-      const int next = i + 1 < count ? s_list[i + 1] & 0x7fffffff : -1;
-      if (next >= 0) fetch(next);
-      im_c16 sc[2];
+    int bands = 1;
+    for (int band = 0; band < bands; ++band) {
+      int my_e = 127;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        sc[t] = pg_zero16();
+      for (int d = 0; d < 4; ++d) {
+        const int hi = max(max(s_scale[0][d][0], s_scale[1][d][0]), max(s_scale[2][d][0], s_scale[3][d][0]));
+        const int lo = min(min(s_scale[0][d][1], s_scale[1][d][1]), min(s_scale[2][d][1], s_scale[3][d][1]));
+        const int mine = hi > 0 ? min((hi - lo) / PG_BAND + 1, PG_BANDS) : 1;   // (what is 2^115 below the largest counts as 0)
+        bands = max(bands, mine);
+        const int e = hi > 0 ? hi - PG_BAND * min(band, mine - 1) : 127;
+        if (d == l16 >> 2) my_e = band < mine ? e : -PG_BAND;   // (a block without scales in this band: all are taken as 0)
+        if (e != e_was[d]) {   // o goes over to these units
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          const im_bf8 kf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_k[buf][pg_k_at(32 * t + l32, 2 * s + half)]);
-          sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc[t], 0, 0, 0);
+          for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_was[d] - e);
+          e_was[d] = e;
         }
       }
-      if (entry < 0) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int key = 32 * t + 8 * g + 4 * half;
-            int4 at = make_int4(0, 0, 0, 0);
-            if (a.q_pos) at = *(const int4*)&s_pos[buf][key];
-            sc[t][4 * g + 0] = key + 0 < nk && at.x <= q_pos ? sc[t][4 * g + 0] : -INFINITY;
-            sc[t][4 * g + 1] = key + 1 < nk && at.y <= q_pos ? sc[t][4 * g + 1] : -INFINITY;
-            sc[t][4 * g + 2] = key + 2 < nk && at.z <= q_pos ? sc[t][4 * g + 2] : -INFINITY;
-            sc[t][4 * g + 3] = key + 3 < nk && at.w <= q_pos ? sc[t][4 * g + 3] : -INFINITY;
-          }
-      }
-      float top = sc[0][0];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[t][r]);
-      top = halves_max_f(top);
-      if (__any(top > m)) {
-        const float m_new = fmaxf(m, top), f = __builtin_amdgcn_exp2f((m - m_new) * c2);
-        m = m_new;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= f;
-      }
-      const float mc = m * c2;
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          sc[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], c2, -mc));
-          sum += sc[t][r];
-        }
-      l += sum;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {   // 16 keys
-        float pr[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) pr[r] = sc[t >> 1][8 * (t & 1) + r];
-        im_bf8 ph, pl;
-        pg_split8(pr, ph, pl);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const im_bf8 vf = __builtin_bit_cast(im_bf8, *(const uint4*)&s_v[buf][pg_v_at(32 * d + l32, 2 * t + half)]);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, o[d], 0, 0, 0);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph, o[d], 0, 0, 0);
-        }
-      }
-      if (s_odd[buf][0] | s_odd[buf][1] | s_odd[buf][2] | s_odd[buf][3]) {   // blocks of NaN: for the rows that see them
-        const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
-        for (int key = 0; key < min(nk, PG_SLOTS); ++key) {
-          uint32_t blocks = 0;
-          for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
-          if (blocks && (!a.q_pos || s_pos[buf][key] <= q_pos)) nan_blocks |= blocks;
-        }
-      }
-      if (next >= 0) store(next, buf ^ 1);
-      __syncthreads();
+      segment(count, my_e, band == 0);
     }
   }
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_was[d] - 127);
   l = halves_sum_f(l);
 
   if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_combine

@@ -520,3 +520,20 @@ def test_calls_give_the_same_bits_each_time_on_any_stream():
                 im.im_attn_packed_with_readout(p.h, p.p, p.st, q[:, :n_q].contiguous(), out, qp[:, :n_q].contiguous())
                 torch.cuda.synchronize()
                 assert torch.equal(out, want.setdefault(n_q, out))
+
+
+@pytest.mark.parametrize("spread", [2.0 ** 10, 2.0 ** 26, 2.0 ** 60])
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_values_of_very_different_size(n_q, spread):
+    """Queries that see the small values alone get them as exactly as if there were no others."""
+    p = Pair(batch=1, heads=(4, 2), capacity=300)
+    v = p.bf(1, 2, 280, 128)
+    small = torch.arange(280) < 140
+    v[:, :, small] = (v[:, :, small].float() / spread).bfloat16()
+    v[:, :, 30, 32:64] *= 2.0 ** -40           # smaller still, in one block
+    p.append(280, v=v)
+    p.attend(n_q, q_pos=np.full((1, n_q), 139))
+    p.attend(n_q, q_pos=np.full((1, n_q), 279))
+    p.attend(n_q, q_pos=np.linspace(0, 279, n_q).astype(int)[None])
+    p.memory()
+    p.attend(n_q, q_pos=np.linspace(100, 279, n_q).astype(int)[None])
