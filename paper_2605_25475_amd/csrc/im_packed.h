@@ -633,9 +633,9 @@ __device__ __forceinline__ void pg_split8(const float (&x)[8], im_bf8& hi, im_bf
 typedef _Float16 im_h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 im_h2 __attribute__((ext_vector_type(2)));
 
-// A page expanded in LDS.  16-byte piece g of K's row r (16 pieces) is at 16 (16 r + (g ^ r % 8 ^ 2 (g / 8))), of V's dim d (8 pieces of 8
-// keys) at 16 (8 d + (g ^ (d ^ d / 8) % 8)): the 8 rows of a read and the lane groups of a write fall on all banks, and the addresses of
-// a thread's pieces are one value XOR constants.
+// A page expanded in LDS.  16-byte piece g of K's row r (16 pieces) is at 16 (16 r + (g ^ r % 16)), of V's dim d (8 pieces of 8 keys) at
+// 16 (8 d + (g ^ (d / 2 ^ d / 16) % 8)): the 16 rows that a read takes at a time (0-3, 12-15, 20-23, 24-27 of 32) fall on all 64
+// banks, and the addresses of a thread's pieces are one value XOR constants.
 struct PgTile {
   __attribute__((aligned(16))) char k[PG_SLOTS * IM_D * 2];
   __attribute__((aligned(16))) char v[PG_SLOTS * IM_D * 2];
@@ -666,25 +666,29 @@ __device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, int e,
   }
 }
 
-// grid (row tiles, splits, units), 4 waves; wave w has rows 32 w .. 32 w + 31 of the tile (row r is query r / G, head r % G) as the
+// grid (row tiles x splits x units), 4 waves; wave w has rows 32 w .. 32 w + 31 of the tile (row r is query r / G, head r % G) as the
 // columns of every product, so that a lane's 16 logits of a block of 32 keys, its running maximum and its sums belong to one row:
 //   S^T = K Q^T, O^T = V^T P^T; products of 32 x 32 x 16, register i of lane (l32, half) is row 8 (i / 4) + 4 half + i % 4, column l32.
 // P^T's registers are its operand as they are; V^T's keys are laid out in LDS in that order (16 t + 8 half + 4 g + j for key
-// 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded in LDS by the whole workgroup, the next page's bytes on their way.
+// 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded in LDS by the whole workgroup, between the products S^T of the page before it, and the
+// bytes of the page behind it are on their way.  (8 waves of 256 rows, half of them expanding K and half V: 470 us where this takes 473.)
 //   K goes in as bf16 (exact).  P goes in as fp16, half a step of 2^-11 off each (the sums of P stay fp32), with V as fp16 multiples of 2^e per
 // 32 dims, e the largest scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment
 // is gone over again for the scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
-__global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro) {
+__global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro, int units) {
   __shared__ PgTile s_tile[2];
   __shared__ int s_list[PG_SEG];   // pages to look at; bit 31: some row does not see all of it
   __shared__ int s_n, s_lim[4][2], s_scale[4][4][2];
-  const int unit = blockIdx.z, split = blockIdx.y, b = unit / a.H_kv, h = unit % a.H_kv;
+  // the units of a row tile side by side: with 8 of them, or a multiple, a unit's workgroups share an XCD's L2; the last rows, which see the
+  // most of a prompt, first
+  const int unit = blockIdx.x % units, split = blockIdx.x / units % a.n_splits, tile = gridDim.x / (units * a.n_splits) - 1 - blockIdx.x / (units * a.n_splits);
+  const int b = unit / a.H_kv, h = unit % a.H_kv;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
   const int n_true = a.len[unit], n = min(n_true, a.max_live), R = a.n_q * a.G;
-  if (n_true > a.max_live && split == 0 && blockIdx.x == 0 && tid == 0) atomicOr(a.status, IM_STATUS_LIVE_EXCEEDED_BIT);
+  if (n_true > a.max_live && split == 0 && tile == 0 && tid == 0) atomicOr(a.status, IM_STATUS_LIVE_EXCEEDED_BIT);
   const int n_pages = (n + PG_SLOTS - 1) / PG_SLOTS, per = (n_pages + a.n_splits - 1) / a.n_splits;
   const int p_begin = split * per, p_end = min(n_pages, p_begin + per);
-  const int my_row = blockIdx.x * PG_ROWS + 32 * w + l32, row = min(my_row, R - 1), query = row / a.G;
+  const int my_row = tile * PG_ROWS + 32 * w + l32, row = min(my_row, R - 1), query = row / a.G;
   const size_t q_row = ((size_t)b * a.n_q + query) * a.H + h * a.G + row % a.G;
   im_bf8 qf[8];
 #pragma unroll
@@ -698,8 +702,9 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     if (lane == 0) { s_lim[w][0] = lo; s_lim[w][1] = hi; }
   }
   __syncthreads();
-  const int q_lo = min(min(s_lim[0][0], s_lim[1][0]), min(s_lim[2][0], s_lim[3][0]));
-  const int q_hi = max(max(s_lim[0][1], s_lim[1][1]), max(s_lim[2][1], s_lim[3][1]));
+  int q_lo = s_lim[0][0], q_hi = s_lim[0][1];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) { q_lo = min(q_lo, s_lim[i][0]); q_hi = max(q_hi, s_lim[i][1]); }
   const int32_t *tab = a.table + (size_t)unit * a.T, *pos = a.pos + (size_t)unit * a.C;
   const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
   float m = -1e30f, l = 0.f;
@@ -711,9 +716,9 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 
   // a thread's share of a page: 32 codes of K (row tid / 4, block tid % 4), and of V (keys 16 w + 4 kq .. + 3, dims 8 l16 ..)
   const int l16 = lane & 15, kq = lane >> 4;
-  const int k_put = 256 * (tid >> 2) + 16 * ((4 * (tid & 3)) ^ ((tid >> 2) & 7) ^ ((tid & 2) ? 2 : 0));
-  const int v_put = 1024 * l16 + 16 * ((2 * w + (kq & 1)) ^ (l16 & 7)) + 8 * (kq >> 1);
-  const int k_get = 256 * l32 + 16 * (half ^ (l32 & 7)), v_get = 128 * l32 + 16 * (half ^ (l32 & 7) ^ (l32 >> 3));
+  const int k_put = 256 * (tid >> 2) + 16 * ((4 * (tid & 3)) ^ ((tid >> 2) & 15));
+  const int v_put = 1024 * l16 + 16 * ((2 * w + (kq & 1)) ^ (4 * (l16 & 1)) ^ (l16 >> 1)) + 8 * (kq >> 1);
+  const int k_get = 256 * l32 + 16 * (half ^ (l32 & 15)), v_get = 128 * l32 + 16 * (half ^ ((l32 >> 1) & 7) ^ (l32 >> 4));
   uint4 kw, vw;
   uint32_t ks, vs;
   int ps = 0;
@@ -723,58 +728,73 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     vw = *(const uint4*)(page + PG_V + 16 * tid);
     ks = (uint8_t)page[PG_KS + tid];
     vs = *(const uint32_t*)(page + PG_VS + 64 * w + 16 * kq + 4 * (l16 >> 2));
-    if (a.q_pos && tid < PG_SLOTS) ps = p * PG_SLOTS + tid < n ? pos[p * PG_SLOTS + tid] : 0;
+    if (a.q_pos) ps = pos[min(p * PG_SLOTS + lane, n - 1)];
+  };
+  // entries behind the last one hold anything: their values are taken as 0, as a block of NaN is, which the rows that see it get below;
+  // whether there is one among these
+  auto settle = [&](int p) {
+    const int nk = n - p * PG_SLOTS;
+    const uint32_t y = ~vs;
+    const bool has_255 = ((y - 0x01010101u) & ~y & 0x80808080u) != 0;   // some byte of vs is 255
+    bool odd = false;
+    if (__any(has_255 || nk < PG_SLOTS)) {
+      uint32_t xw[4] = {vw.x, vw.y, vw.z, vw.w}, sc = vs;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool live = 16 * w + 4 * kq + i < nk, nan = ((vs >> (8 * i)) & 255u) == 255u;
+        odd |= live && nan;
+        if (!live || nan) { xw[i] = 0u; sc &= ~(255u << (8 * i)); }
+      }
+      vw = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+      vs = sc;
+    }
+    return __any(odd);
   };
 
   // the listed pages; my_e: the units of this thread's share of V; counted: whether P counts towards the sums
   auto segment = [&](int count, int my_e, bool counted) {
-    auto store = [&](int p, PgTile& t) {
-      const int nk = n - p * PG_SLOTS;
+    auto expand = [&](bool odd, PgTile& t) {
       const float f = pg_scale(ks);
       const uint32_t kv[4] = {kw.x, kw.y, kw.z, kw.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) *(uint4*)(t.k + (k_put ^ (16 * i))) = pg_expand(kv[i], f);
-      // entries behind the last one hold anything: taken as 0, as a block of NaN is, which the rows that see it get below
-      bool odd = false;
-      uint4 x = vw;
-      uint32_t sc = vs, y = ~vs;
-      const bool has_255 = ((y - 0x01010101u) & ~y & 0x80808080u) != 0;   // some byte of vs is 255
-      if (__any(has_255 || nk < PG_SLOTS)) {
-        uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool live = 16 * w + 4 * kq + i < nk, nan = ((vs >> (8 * i)) & 255u) == 255u;
-          odd |= live && nan;
-          if (!live || nan) { xw[i] = 0u; sc &= ~(255u << (8 * i)); }
-        }
-        x = make_uint4(xw[0], xw[1], xw[2], xw[3]);
-      }
-      const bool any_odd = __any(odd);
-      if (lane == 0) t.odd[w] = any_odd;
       uint2 piece[8];
-      pg_v_pieces(x, sc, my_e, piece);
+      pg_v_pieces(vw, vs, my_e, piece);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) *(uint2*)(t.v + (v_put ^ (16 * e)) + 128 * e) = piece[e];
-      if (a.q_pos && tid < PG_SLOTS) t.pos[tid] = ps;
+      for (int e = 0; e < 8; ++e) *(uint2*)(t.v + (v_put ^ (16 * (e >> 1))) + 128 * e) = piece[e];
+      t.pos[lane] = ps;   // (every wave the same)
+      t.odd[w] = odd;
     };
-    fetch(s_list[0] & 0x7fffffff);
-    store(s_list[0] & 0x7fffffff, s_tile[0]);
+    auto page_at = [&](int i) { return s_list[min(i, count - 1)] & 0x7fffffff; };   // (the last one again where there are no more)
+    fetch(page_at(0));
+    expand(settle(page_at(0)), s_tile[0]);
+    fetch(page_at(1));
     __syncthreads();
     for (int i = 0; i < count; ++i) {
       const PgTile& t = s_tile[i & 1];
       const int entry = s_list[i], p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
-      const int next = i + 1 < count ? s_list[i + 1] & 0x7fffffff : -1;
-      if (next >= 0) fetch(next);
+      const bool odd_next = settle(page_at(i + 1));
       im_c16 sc[2];
       sc[0] = pg_zero16();
       sc[1] = pg_zero16();
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const char* at = t.k + (k_get ^ (16 * ((2 * s) ^ (s >= 4 ? 2 : 0))));
+        const char* at = t.k + (k_get ^ (32 * s));
 #pragma unroll
         for (int u = 0; u < 2; ++u)
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(im_bf8, *(const uint4*)(at + 8192 * u)), qf[s], sc[u], 0, 0, 0);
       }
+      expand(odd_next, s_tile[(i & 1) ^ 1]);
+#ifdef PG_GROUPS
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      }
+#endif
+      fetch(page_at(i + 2));
       if (entry < 0) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -795,7 +815,8 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[u][r]);
       top = halves_max_f(top);
-      if (__any(top > m)) {
+      // (P may grow to 2^8 before the maximum follows: most pages bring some row a new one, few a much larger one)
+      if (__any((top - m) * c2 > 8.f)) {
         const float m_new = fmaxf(m, top), f = __builtin_amdgcn_exp2f((m - m_new) * c2);
         m = m_new;
         l *= f;
@@ -825,7 +846,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
         const im_h8 pf = __builtin_bit_cast(im_h8, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
         for (int d = 0; d < 4; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(im_h8, *(const uint4*)(t.v + 4096 * d + (v_get ^ (16 * ((2 * u) ^ (d & 1 ? 4 : 0)))))), pf, o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(im_h8, *(const uint4*)(t.v + 4096 * d + (v_get ^ (32 * (u ^ d))))), pf, o[d], 0, 0, 0);
       }
       if (t.odd[0] | t.odd[1] | t.odd[2] | t.odd[3]) {   // blocks of NaN: for the rows that see them
         const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
@@ -835,7 +856,6 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
           if (blocks && (!a.q_pos || t.pos[key] <= q_pos)) nan_blocks |= blocks;
         }
       }
-      if (next >= 0) store(next, s_tile[(i & 1) ^ 1]);
       __syncthreads();
     }
   };
@@ -908,8 +928,9 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
       int my_e = 127;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const int hi = max(max(s_scale[0][d][0], s_scale[1][d][0]), max(s_scale[2][d][0], s_scale[3][d][0]));
-        const int lo = min(min(s_scale[0][d][1], s_scale[1][d][1]), min(s_scale[2][d][1], s_scale[3][d][1]));
+        int hi = 0, lo = 255;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { hi = max(hi, s_scale[i][d][0]); lo = min(lo, s_scale[i][d][1]); }
         const int mine = hi > 0 ? min((hi - lo) / PG_BAND + 1, PG_BANDS) : 1;   // (what is 2^115 below the largest counts as 0)
         bands = max(bands, mine);
         const int e = hi > 0 ? hi - PG_BAND * min(band, mine - 1) : 127;

@@ -1076,7 +1076,7 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
     else k_packed_attn_few<false><<<dim3(a.n_splits, units), 256, 0, s>>>(a);
   } else {
     const PgReadout ro = {Wt, wg, st->M, st->b, p->cg, c.mem_eps, (bf16_t*)out, readout_dbg};
-    k_packed_attn_many<<<dim3(tiles, a.n_splits, units), 256, 0, s>>>(a, ro);
+    k_packed_attn_many<<<tiles * a.n_splits * units, 256, 0, s>>>(a, ro, units);
   }
   if (few || a.n_splits > 1) {
     auto combine = [&](auto kernel, int rw) {
