@@ -636,24 +636,23 @@ typedef _Float16 im_h2 __attribute__((ext_vector_type(2)));
 // A page expanded in LDS.  16-byte piece g of K's row r (16 pieces) is at 16 (16 r + (g ^ r % 16)), of V's dim d (8 pieces of 8 keys) at
 // 16 (8 d + (g ^ (d / 2 ^ d / 16) % 8)): the 16 rows that a read takes at a time (0-3, 12-15, 20-23, 24-27 of 32) fall on all 64
 // banks, and the addresses of a thread's pieces are one value XOR constants.
-struct PgTile {
-  __attribute__((aligned(16))) char k[PG_SLOTS * IM_D * 2];
-  __attribute__((aligned(16))) char v[PG_SLOTS * IM_D * 2];
+#define PG_TILE 32768
+#define PG_TILE_V 16384   // V behind K
+struct PgTile {   // what goes with a tile
   __attribute__((aligned(16))) int pos[PG_SLOTS];
   int odd[4];   // whether the wave's 16 keys hold a block of NaN
 };
 
-// 4 keys x 8 dims of V (a word of codes and a scale byte per key) -> 8 pieces of 4 keys, fp16 values in units of 2^(e - 127).  Scales of
-// e - 22 .. e are taken (exact: a code is at least 0.5), others as 0.
+// 4 keys x 8 dims of V (a word of codes and a scale byte per key) -> 8 pieces of 4 keys, fp16 values in units of 2^(e - 127); unit = 2^(127 - e).
+// Exact for scales of e - 22 .. e (a code is at least 0.5); a scale byte of 0 gives 0.
 #define PG_BAND 23
 #define PG_BANDS 5
-__device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, int e, uint2 (&piece)[8]) {
-  const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w};
+__device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, float unit, uint2 (&piece)[8]) {
+  const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w}, sc[4] = {vs << 23, (vs << 15) & 0x7f800000u, (vs << 7) & 0x7f800000u, (vs >> 1) & 0x7f800000u};
   uint32_t x[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int byte = (vs >> (8 * i)) & 255u;
-    const float f = (uint32_t)(e - byte) < PG_BAND ? pg_scale(byte + 127 - e) : 0.f;
+    const float f = __uint_as_float(sc[i]) * unit;
     x[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 0));
     x[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 1));
     x[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], f, 2));
@@ -676,7 +675,8 @@ __device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, int e,
 // 32 dims, e the largest scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment
 // is gone over again for the scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
 __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro, int units) {
-  __shared__ PgTile s_tile[2];
+  __shared__ __attribute__((aligned(16))) char s_tile[2 * PG_TILE];
+  __shared__ PgTile s_extra[2];
   __shared__ int s_list[PG_SEG];   // pages to look at; bit 31: some row does not see all of it
   __shared__ int s_n, s_lim[4][2], s_scale[4][4][2];
   // the units of a row tile side by side: with 8 of them, or a multiple, a unit's workgroups share an XCD's L2; the last rows, which see the
@@ -716,13 +716,14 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 
   // a thread's share of a page: 32 codes of K (row tid / 4, block tid % 4), and of V (keys 16 w + 4 kq .. + 3, dims 8 l16 ..)
   const int l16 = lane & 15, kq = lane >> 4;
-  const int k_put = 256 * (tid >> 2) + 16 * ((4 * (tid & 3)) ^ ((tid >> 2) & 15));
-  const int v_put = 1024 * l16 + 16 * ((2 * w + (kq & 1)) ^ (4 * (l16 & 1)) ^ (l16 >> 1)) + 8 * (kq >> 1);
-  const int k_get = 256 * l32 + 16 * (half ^ (l32 & 15)), v_get = 128 * l32 + 16 * (half ^ ((l32 >> 1) & 7) ^ (l32 >> 4));
+  // (LDS addresses as offsets in s_tile; they change tiles by an XOR with the tile's size)
+  uint32_t k_put = 256 * (tid >> 2) + 16 * ((4 * (tid & 3)) ^ ((tid >> 2) & 15));
+  uint32_t v_put = PG_TILE_V + 1024 * l16 + 16 * ((2 * w + (kq & 1)) ^ (4 * (l16 & 1)) ^ (l16 >> 1)) + 8 * (kq >> 1);
+  uint32_t k_get = 256 * l32 + 16 * (half ^ (l32 & 15)), v_get = PG_TILE_V + 128 * l32 + 16 * (half ^ ((l32 >> 1) & 7) ^ (l32 >> 4));
   uint4 kw, vw;
   uint32_t ks, vs;
   int ps = 0;
-  auto fetch = [&](int p) {
+  auto fetch = [&](int p) {   // (p is uniform: the page's address is in scalar registers, the thread's offset in one that stays)
     const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
     kw = *(const uint4*)(page + 16 * tid);
     vw = *(const uint4*)(page + PG_V + 16 * tid);
@@ -730,70 +731,66 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     vs = *(const uint32_t*)(page + PG_VS + 64 * w + 16 * kq + 4 * (l16 >> 2));
     if (a.q_pos) ps = pos[min(p * PG_SLOTS + lane, n - 1)];
   };
-  // entries behind the last one hold anything: their values are taken as 0, as a block of NaN is, which the rows that see it get below;
-  // whether there is one among these
-  auto settle = [&](int p) {
-    const int nk = n - p * PG_SLOTS;
-    const uint32_t y = ~vs;
-    const bool has_255 = ((y - 0x01010101u) & ~y & 0x80808080u) != 0;   // some byte of vs is 255
-    bool odd = false;
-    if (__any(has_255 || nk < PG_SLOTS)) {
-      uint32_t xw[4] = {vw.x, vw.y, vw.z, vw.w}, sc = vs;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool live = 16 * w + 4 * kq + i < nk, nan = ((vs >> (8 * i)) & 255u) == 255u;
-        odd |= live && nan;
-        if (!live || nan) { xw[i] = 0u; sc &= ~(255u << (8 * i)); }
-      }
-      vw = make_uint4(xw[0], xw[1], xw[2], xw[3]);
-      vs = sc;
-    }
-    return __any(odd);
-  };
 
-  // the listed pages; my_e: the units of this thread's share of V; counted: whether P counts towards the sums
-  auto segment = [&](int count, int my_e, bool counted) {
+  // the listed pages; my_e: the units of this thread's share of V (2^(my_e - 127)); bands: times that the segment is gone over, this is the band-th
+  auto segment = [&](int count, int my_e, int band, int bands) {
+    const float unit = pg_scale(254 - max(my_e, 1));   // 2^(127 - my_e)
+    // Entries behind the last one hold anything: their values are taken as 0, as a block of NaN is, which the rows that see it get below,
+    // and what belongs to another band.  Whether there is NaN among these.
+    auto settle = [&](int p) {
+      const int nk = n - p * PG_SLOTS;
+      const uint32_t y = ~vs;
+      const bool has_255 = ((y - 0x01010101u) & ~y & 0x80808080u) != 0;   // some byte of vs is 255
+      bool odd = false;
+      if (nk < PG_SLOTS || bands > 1 || __any(has_255)) {
+        uint32_t sc = vs;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t byte = (vs >> (8 * i)) & 255u;
+          const bool live = 16 * w + 4 * kq + i < nk, nan = byte == 255u;
+          odd |= live && nan;
+          if (!live || nan || (bands > 1 && (uint32_t)(my_e - (int)byte) >= PG_BAND)) sc &= ~(255u << (8 * i));
+        }
+        vs = sc;
+      }
+      return __any(odd);
+    };
     auto expand = [&](bool odd, PgTile& t) {
       const float f = pg_scale(ks);
       const uint32_t kv[4] = {kw.x, kw.y, kw.z, kw.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *(uint4*)(t.k + (k_put ^ (16 * i))) = pg_expand(kv[i], f);
+      for (int i = 0; i < 4; ++i) *(uint4*)((char*)s_tile + (k_put ^ (16 * i))) = pg_expand(kv[i], f);
       uint2 piece[8];
-      pg_v_pieces(vw, vs, my_e, piece);
+      pg_v_pieces(vw, vs, unit, piece);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) *(uint2*)(t.v + (v_put ^ (16 * (e >> 1))) + 128 * e) = piece[e];
+      for (int e = 0; e < 8; ++e) *(uint2*)((char*)s_tile + (v_put ^ (16 * (e >> 1))) + 128 * e) = piece[e];
+      k_put ^= PG_TILE;
+      v_put ^= PG_TILE;
       t.pos[lane] = ps;   // (every wave the same)
       t.odd[w] = odd;
     };
-    auto page_at = [&](int i) { return s_list[min(i, count - 1)] & 0x7fffffff; };   // (the last one again where there are no more)
+    auto entry_at = [&](int i) { return __builtin_amdgcn_readfirstlane(s_list[min(i, count - 1)]); };   // (the last one again where there are no more)
+    auto page_at = [&](int i) { return entry_at(i) & 0x7fffffff; };
     fetch(page_at(0));
-    expand(settle(page_at(0)), s_tile[0]);
+    expand(settle(page_at(0)), s_extra[0]);
     fetch(page_at(1));
     __syncthreads();
     for (int i = 0; i < count; ++i) {
-      const PgTile& t = s_tile[i & 1];
-      const int entry = s_list[i], p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
+      const PgTile& t = s_extra[i & 1];
+      const int entry = entry_at(i), p = entry & 0x7fffffff, nk = n - p * PG_SLOTS;
       const bool odd_next = settle(page_at(i + 1));
       im_c16 sc[2];
       sc[0] = pg_zero16();
       sc[1] = pg_zero16();
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const char* at = t.k + (k_get ^ (32 * s));
+        const char* at = (const char*)s_tile + (k_get ^ (32 * s));
 #pragma unroll
         for (int u = 0; u < 2; ++u)
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(im_bf8, *(const uint4*)(at + 8192 * u)), qf[s], sc[u], 0, 0, 0);
       }
-      expand(odd_next, s_tile[(i & 1) ^ 1]);
-#ifdef PG_GROUPS
-#pragma unroll
-      for (int s = 0; s < 16; ++s) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
-        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-      }
-#endif
+      k_get ^= PG_TILE;
+      expand(odd_next, s_extra[(i & 1) ^ 1]);
       fetch(page_at(i + 2));
       if (entry < 0) {
 #pragma unroll
@@ -828,26 +825,23 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
       const float mc = m * c2;
       float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          sc[u][r] = __builtin_amdgcn_exp2f(fmaf(sc[u][r], c2, -mc));
-          sum[u] += sc[u][r];
-        }
-      l += counted ? sum[0] + sum[1] : 0.f;
-#pragma unroll
       for (int u = 0; u < 4; ++u) {   // 16 keys
-        float pr[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) pr[r] = sc[u >> 1][8 * (u & 1) + r];
         uint32_t x[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{pr[2 * r], pr[2 * r + 1]}), im_h2));
+        for (int r = 0; r < 4; ++r) {
+          const int at = 8 * (u & 1) + 2 * r;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[u >> 1][at], c2, -mc)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[u >> 1][at + 1], c2, -mc));
+          const im_h2 pk = __builtin_convertvector((im_f2{p0, p1}), im_h2);
+          sum[r & 1] = __builtin_amdgcn_fdot2(pk, im_h2{(_Float16)1.f, (_Float16)1.f}, sum[r & 1], false);   // (the sums of P as it goes in, in fp32)
+          x[r] = __builtin_bit_cast(uint32_t, pk);
+        }
         const im_h8 pf = __builtin_bit_cast(im_h8, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
         for (int d = 0; d < 4; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(im_h8, *(const uint4*)(t.v + 4096 * d + (v_get ^ (32 * (u ^ d))))), pf, o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(im_h8, *(const uint4*)((const char*)s_tile + 4096 * d + (v_get ^ (32 * (u ^ d))))), pf, o[d], 0, 0, 0);
       }
+      v_get ^= PG_TILE;
+      l += band == 0 ? sum[0] + sum[1] : 0.f;
       if (t.odd[0] | t.odd[1] | t.odd[2] | t.odd[3]) {   // blocks of NaN: for the rows that see them
         const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
         for (int key = 0; key < min(nk, PG_SLOTS); ++key) {
@@ -858,6 +852,8 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
       }
       __syncthreads();
     }
+    k_put ^= PG_TILE;   // (writing was a tile ahead of reading)
+    v_put ^= PG_TILE;
   };
 
   for (int seg = p_begin; seg < p_end; seg += PG_SEG) {
@@ -941,7 +937,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
           e_was[d] = e;
         }
       }
-      segment(count, my_e, band == 0);
+      segment(count, my_e, band, bands);
     }
   }
 #pragma unroll
