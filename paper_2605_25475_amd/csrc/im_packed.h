@@ -862,25 +862,22 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     // values per block: lane (key / 4, block) looks at 4 keys; 4 pages of a wave at a time
     int s_hi = 0, s_lo = 255;
     __syncthreads();
-    for (int i0 = 4 * w; i0 < n_seg; i0 += 16) {
-      int id[4], at[4];
-      uint32_t sv[4];
+    // wave w takes pages 8 w .. 8 w + 7 of every 32, all of their bytes together; lane j of a wave knows the number of its j-th page
+    const int my_page = seg + min(32 * (lane >> 3) + 8 * w + (lane & 7), n_seg - 1);
+    const int ids_a = tab[my_page], ids_b = n_seg > 256 ? tab[min(my_page + 256, seg + n_seg - 1)] : 0;
+    for (int i0 = 8 * w, k = 0; i0 < n_seg; i0 += 32, k += 8) {
+      int id[8], at[8];
+      uint32_t sv[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int p = seg + min(i0 + j, n_seg - 1);
-        id[j] = tab[p];
-        at[j] = a.q_pos ? pos[min(p * PG_SLOTS + lane, n - 1)] : 0;
+      for (int j = 0; j < 8; ++j) {
+        id[j] = k < 64 ? __builtin_amdgcn_readlane(ids_a, (k + j) & 63) : __builtin_amdgcn_readlane(ids_b, (k + j) & 63);
+        if (!pg_is_page(id[j], a.n_pages)) id[j] = -1;   // (a table entry that names no page: nothing is there)
+        const char* page = a.pages + (size_t)max(id[j], 0) * PG_BYTES;
+        sv[j] = *(const uint32_t*)(page + PG_VS + 4 * lane);
+        at[j] = a.q_pos ? pos[min((seg + min(i0 + j, n_seg - 1)) * PG_SLOTS + lane, n - 1)] : 0;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!pg_is_page(id[j], a.n_pages)) {   // (a table entry that names no page: nothing is there)
-          if (lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
-          id[j] = -1;
-        }
-        sv[j] = *(const uint32_t*)(a.pages + (size_t)max(id[j], 0) * PG_BYTES + PG_VS + 4 * lane);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 8; ++j) {
         const int i = i0 + j, first = (seg + i) * PG_SLOTS;
         if (i >= n_seg) break;
         int entry = seg + i;
@@ -890,13 +887,16 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
           if (!__any(live && at[j] <= q_hi)) entry = -1;
           else if (__any(live && at[j] > q_lo)) entry |= 1 << 31;
         }
-        if (id[j] < 0) entry = -1;
+        if (id[j] < 0) {
+          if (lane == 0) atomicOr(a.status, IM_STATUS_BAD_PAGE_BIT);
+          entry = -1;
+        }
         if (lane == 0) s_list[i] = entry;
         if (entry == -1) continue;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int byte = (sv[j] >> (8 * k)) & 255u;
-          const bool counts = byte != 255 && byte > 1 && first + 4 * (lane >> 2) + k < n;
+        for (int b4 = 0; b4 < 4; ++b4) {
+          const int byte = (sv[j] >> (8 * b4)) & 255u;
+          const bool counts = byte != 255 && byte > 1 && first + 4 * (lane >> 2) + b4 < n;
           s_hi = counts ? max(s_hi, byte) : s_hi;
           s_lo = counts ? min(s_lo, byte) : s_lo;
         }
@@ -959,9 +959,17 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     return;
   }
 
-  // the memory readout of the wave's rows: phi^T = Wtheta Q^T, then M^T phi^T with phi and M as two bf16 parts each (2^-16)
+  // the memory readout of the wave's rows: phi^T = Wtheta Q^T, then M^T phi^T with phi and M as two bf16 parts each (2^-16).  Wtheta, then M's parts go
+  // through LDS, once for the four waves (each reading them from the cache by itself: 20 us more of 16384 rows x 8 units): row r's 16-byte
+  // piece g at 16 (16 r + (g ^ r % 16)), M by dims with its rows in the order of phi's registers.
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float* Mu = ro.M + (size_t)unit * IM_DM * IM_D;
+  auto piece_at = [&](int r, int g) { return s_tile + 256 * r + 16 * (g ^ (r & 15)); };
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = tid + 256 * i;
+    *(uint4*)piece_at(at >> 4, at & 15) = *(const uint4*)(ro.Wtheta + 8 * at);
+  }
   float den = 0.f, gz = 0.f;
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
@@ -970,15 +978,14 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 #pragma unroll
     for (int e = 0; e < 4; ++e) gz = fmaf(bf_lo(xw[e]), bf_lo(yw[e]), fmaf(bf_hi(xw[e]), bf_hi(yw[e]), gz));
   }
+  __syncthreads();
   im_bf8 ph[8], pl[8];   // operand of 16 values of phi each
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) {
     im_c16 phi = pg_zero16();
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const im_bf8 wf = __builtin_bit_cast(im_bf8, *(const uint4*)(ro.Wtheta + (32 * cb + l32) * IM_D + 16 * s + 8 * half));
-      phi = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, qf[s], phi, 0, 0, 0);
-    }
+    for (int s = 0; s < 8; ++s)
+      phi = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(im_bf8, *(const uint4*)piece_at(32 * cb + l32, 2 * s + half)), qf[s], phi, 0, 0, 0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) den = fmaf(phi[r] * phi[r], ro.b[(size_t)unit * IM_DM + 32 * cb + 8 * (r >> 2) + 4 * half + (r & 3)], den);
 #pragma unroll
@@ -991,16 +998,32 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   }
   den = halves_sum_f(den) + ro.mem_eps;
   const float gate = 1.f / (1.f + __expf(-(halves_sum_f(gz) + ro.cg))) / den;
+  __syncthreads();
+  // rows 4 c .. 4 c + 3 of M, of one dim: half of piece 2 (c / 4) + c % 2, its first half for c % 4 < 2
+#pragma unroll 4
+  for (int i = 0; i < 16; ++i) {
+    const int dim = tid & 127, c = 2 * i + (tid >> 7);
+    float x[4];
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = Mu[(4 * c + r) * IM_D + dim];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      hi[r] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{x[2 * r], x[2 * r + 1]}), im_bf2));
+      lo[r] = __builtin_bit_cast(uint32_t, __builtin_convertvector((im_f2{x[2 * r] - bf_lo(hi[r]), x[2 * r + 1] - bf_hi(hi[r])}), im_bf2));
+    }
+    char* at = piece_at(dim, 2 * (c >> 2) + (c & 1)) + 8 * ((c >> 1) & 1);
+    *(uint2*)at = make_uint2(hi[0], hi[1]);
+    *(uint2*)(at + PG_TILE) = make_uint2(lo[0], lo[1]);
+  }
+  __syncthreads();
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
     im_c16 mem = pg_zero16();
 #pragma unroll
     for (int t = 0; t < 8; ++t) {   // 16 of the memory's rows
-      float x[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) x[r] = Mu[(16 * t + 8 * (r >> 2) + 4 * half + (r & 3)) * IM_D + 32 * d + l32];
-      im_bf8 mh, ml;
-      pg_split8(x, mh, ml);
+      const char* at = piece_at(32 * d + l32, 2 * t + half);
+      const im_bf8 mh = __builtin_bit_cast(im_bf8, *(const uint4*)at), ml = __builtin_bit_cast(im_bf8, *(const uint4*)(at + PG_TILE));
       mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ml, ph[t], mem, 0, 0, 0);
       mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mh, pl[t], mem, 0, 0, 0);
       mem = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mh, ph[t], mem, 0, 0, 0);
