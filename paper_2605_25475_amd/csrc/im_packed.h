@@ -302,7 +302,7 @@ struct PgAttn {
   const int32_t *table, *len, *pos;
   const bf16_t* q;
   const int32_t* q_pos;   // NULL: every query sees every entry
-  float* part;            // records [batch][query][head][split]: maximum, denominator, 128 numerators
+  float* part;            // records [batch][query][head][split]: maximum (of log2), denominator, 128 numerators
   int32_t* status;
   int n_pages, T, C, H, H_kv, G, n_q, max_live, n_splits;
   float scale;
@@ -353,6 +353,7 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
   for (int c = 0; c < 4; ++c) qf[c] = *(const uint4*)(a.q + q_row * IM_D + 32 * kq + 8 * c);
   const int q_pos = MASK ? a.q_pos[(size_t)b * a.n_q + query] : 0;
   const int32_t* tab = a.table + (size_t)unit * a.T;
+  const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
   float m = -1e30f, l = 0.f;
   uint32_t nan_blocks = 0;
   im_c4 o[8];
@@ -361,6 +362,11 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
   // the next page's bytes are on their way while a page is worked on
   uint4 kw[4], vw[4], kw_next[4], vw_next[4];
   uint32_t ks[4], vs[4], ks_next[4], vs_next[4];
+  int ps = 0, ps_next = 0, q_lo = q_pos;   // position of the page's entry `lane`; what every row sees is not above q_lo
+  if (MASK) {
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) q_lo = min(q_lo, __shfl_xor(q_lo, d, 64));
+  }
   auto fetch = [&](int p) {   // false: a table entry that names no page: nothing is there
     const int id = tab[p];
     if (!pg_is_page(id, a.n_pages)) {
@@ -378,6 +384,7 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
       vw_next[t] = load_stream16(page + PG_V + 1024 * t + 16 * lane);
       vs_next[t] = *(const uint32_t*)(page + PG_VS + 64 * t + 16 * kq + 4 * (l16 >> 2));
     }
+    if (MASK) ps_next = a.pos[(size_t)unit * a.C + min(p * PG_SLOTS + lane, n - 1)];
     return true;
   };
   int p = split * per + w;
@@ -386,27 +393,37 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
     const bool now = there;
 #pragma unroll
     for (int t = 0; t < 4; ++t) { kw[t] = kw_next[t]; vw[t] = vw_next[t]; ks[t] = ks_next[t]; vs[t] = vs_next[t]; }
+    ps = ps_next;
     there = p + 4 < p_end && fetch(p + 4);
     if (!now) continue;
     const int nk = min(PG_SLOTS, n - p * PG_SLOTS);
-    float s[4][4], tile_max = -INFINITY;
+    float s[4][4], top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const float f = pg_scale(ks[t]);
       const uint4 kf[4] = {pg_expand(kw[t].x, f), pg_expand(kw[t].y, f), pg_expand(kw[t].z, f), pg_expand(kw[t].w, f)};
       const im_c4 acc = att_logits(kf, qf);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = 16 * t + 4 * kq + r;
-        bool seen = key < nk;
-        if (MASK && seen) seen = a.pos[(size_t)unit * a.C + p * PG_SLOTS + key] <= q_pos;
-        s[t][r] = seen ? acc[r] * a.scale : -INFINITY;
-        tile_max = fmaxf(tile_max, s[t][r]);
-      }
+      for (int r = 0; r < 4; ++r) s[t][r] = acc[r];
     }
-    tile_max = rows_max_f(tile_max);
-    if (__any(tile_max > m)) {
-      const float m_new = fmaxf(m, tile_max), f = __expf(m - m_new);
+    if (nk < PG_SLOTS || (MASK && __any(ps > q_lo))) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = 16 * t + 4 * kq + r;
+          const int at = MASK ? __shfl(ps, key, 64) : 0;   // (every lane takes part)
+          const bool seen = key < nk && (!MASK || at <= q_pos);
+          s[t][r] = seen ? s[t][r] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
+    top = rows_max_f(top);
+    if (__any((top - m) * c2 > 8.f)) {   // (P may grow to 2^8 before the maximum follows)
+      const float m_new = fmaxf(m, top), f = __builtin_amdgcn_exp2f((m - m_new) * c2);
       m = m_new;
       l *= f;
 #pragma unroll
@@ -416,35 +433,42 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
         for (int e = 0; e < 8; ++e) o[e][r] *= fr;
       }
     }
-    float sum = 0.f;
+    const float mc = m * c2;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[t][r] = __expf(s[t][r] - m);
-        sum += s[t][r];
+        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c2, -mc));
+        l += s[t][r];
       }
-    l += rows_sum_f(sum);
     // entries behind the last one hold anything: their values are taken as 0; a block of NaN among the others would reach rows that do
     // not see it (0 * NaN): it is taken as 0, too, and remembered for the rows that do
-    bool odd = false;
+    bool has_255 = false;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      uint32_t* wv = (uint32_t*)&vw[t];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t byte = (vs[t] >> (8 * i)) & 255u;
-        const bool live = 16 * t + 4 * kq + i < nk;
-        if (live && byte == 255u) odd = true;
-        if (!live || byte == 255u) { wv[i] = 0u; vs[t] &= ~(255u << (8 * i)); }
-      }
+      const uint32_t y = ~vs[t];
+      has_255 |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
     }
-    if (__any(odd)) {
-      const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
-      for (int key = 0; key < nk; ++key) {
-        uint32_t blocks = 0;
-        for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
-        if (blocks && (!MASK || a.pos[(size_t)unit * a.C + p * PG_SLOTS + key] <= q_pos)) nan_blocks |= blocks;
+    if (nk < PG_SLOTS || __any(has_255)) {
+      bool odd = false;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t wv[4] = {vw[t].x, vw[t].y, vw[t].z, vw[t].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool live = 16 * t + 4 * kq + i < nk, nan = ((vs[t] >> (8 * i)) & 255u) == 255u;
+          odd |= live && nan;
+          if (!live || nan) { wv[i] = 0u; vs[t] &= ~(255u << (8 * i)); }
+        }
+        vw[t] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+      }
+      if (__any(odd)) {
+        const char* page = a.pages + (size_t)tab[p] * PG_BYTES;
+        for (int key = 0; key < nk; ++key) {
+          uint32_t blocks = 0;
+          for (int c = 0; c < 4; ++c) blocks |= (uint8_t)page[pg_v_scale(key, c)] == 255u ? 1u << c : 0u;
+          if (blocks && (!MASK || a.pos[(size_t)unit * a.C + p * PG_SLOTS + key] <= q_pos)) nan_blocks |= blocks;
+        }
       }
     }
 #pragma unroll
@@ -453,15 +477,18 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint4 x = vw[2 * t + u];
-        const uint32_t wv[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t wv[4] = {x.x, x.y, x.z, x.w}, b4 = vs[2 * t + u];
+        const uint32_t sc[4] = {b4 << 23, (b4 << 15) & 0x7f800000u, (b4 << 7) & 0x7f800000u, (b4 >> 1) & 0x7f800000u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vf[u][i] = pg_expand(wv[i], pg_scale((vs[2 * t + u] >> (8 * i)) & 255u));
+        for (int i = 0; i < 4; ++i) vf[u][i] = pg_expand(wv[i], __uint_as_float(sc[i]));
       }
       const float pr[2][4] = {{s[2 * t][0], s[2 * t][1], s[2 * t][2], s[2 * t][3]},
                               {s[2 * t + 1][0], s[2 * t + 1][1], s[2 * t + 1][2], s[2 * t + 1][3]}};
       pg_pv(pr, vf, o);
     }
   }
+  l = rows_sum_f(l);
+  m *= c2;
   if (kq == 0) { s_ml[w][l16][0] = m; s_ml[w][l16][1] = l; s_nan[w][l16] = nan_blocks; }
   att_store(o, &s_acc[w][0][0], l16, kq, min(R, 16));
   __syncthreads();
@@ -472,7 +499,7 @@ __global__ __launch_bounds__(256) void k_packed_attn_few(PgAttn a) {
     uint32_t nb = 0;
 #pragma unroll
     for (int ww = 0; ww < 4; ++ww) {
-      const float f = __expf(s_ml[ww][r][0] - mm);
+      const float f = __builtin_amdgcn_exp2f(s_ml[ww][r][0] - mm);
       ov = fmaf(f, s_acc[ww][r][d], ov);
       lv = fmaf(f, s_ml[ww][r][1], lv);
       nb |= s_nan[ww][r];
@@ -526,12 +553,12 @@ __global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict_
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (c0 + 4 * j < n_splits) top = fmaxf(top, cm[j]);
-      const float f = __expf(m - top);
+      const float f = __builtin_amdgcn_exp2f(m - top);
       l *= f; o *= f; m = top;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (c0 + 4 * j < n_splits) {
-          const float e = __expf(cm[j] - m);
+          const float e = __builtin_amdgcn_exp2f(cm[j] - m);
           l = fmaf(e, cl[j], l);
           o = fmaf(e, co[j], o);
         }
@@ -580,7 +607,7 @@ __global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict_
       float o = 0.f, l = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float f = __expf(s_ml[k][i][0] - m);
+        const float f = __builtin_amdgcn_exp2f(s_ml[k][i][0] - m);
         o = fmaf(f, s_o[k][i][x], o);
         l = fmaf(f, s_ml[k][i][1], l);
       }
@@ -949,7 +976,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_combine
     if (my_row < R) {
       float* rec = a.part + (q_row * a.n_splits + split) * PG_REC;
-      if (half == 0) { rec[0] = m * a.scale; rec[1] = l; }
+      if (half == 0) { rec[0] = m * c2; rec[1] = l; }
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll

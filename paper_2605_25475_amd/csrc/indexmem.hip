@@ -1065,6 +1065,7 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
   a.max_live = h->max_live; a.scale = c.softmax_scale;
   const bool few = rows <= 16;   // (16 records per query head are always there)
   const int tiles = few ? 1 : (rows + PG_ROWS - 1) / PG_ROWS, wave_pages = few ? 4 : 1;
+  // the workgroups of one generation, two per CU.  One query over 8 units x 131072 entries, aiming at 256, 512, 768, 1024: 44.8, 37.6, 44.8, 39.8 us
   int splits = (int)((512 + (long long)tiles * units - 1) / ((long long)tiles * units));
   const int most = (n_pages + wave_pages - 1) / wave_pages;
   if (splits > most) splits = most;
@@ -1083,8 +1084,10 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
       kernel<<<dim3((rows + rw - 1) / rw, units), 512, 0, s>>>(a.part, a.n_splits, (const bf16_t*)q, Wt, wg, p->cg, st->M, st->b, c.n_q_heads,
                                                                c.n_kv_heads, G, n_q, c.mem_eps, (bf16_t*)out, readout_dbg);
     };
-    if (all_rows <= 512 || rows == 1) combine(k_packed_combine<1>, 1);
-    else if (all_rows <= 2048 || rows == 2) combine(k_packed_combine<2>, 2);
+    // rows of a unit per workgroup, which reads the unit's memory once for them; us with 1, 2, 4: 32 rows in all 4.7, 5.5, 7.6; 128 rows 5.3, 6.4, 9.0;
+    // 256 rows 6.1, 6.1, 8.8; 448 rows 9.1, 7.8, 10.1; 512 rows 9.0, 7.3, 9.0; 1024 rows 13.4, 9.9, 8.8; 2048 rows 23.4, 16.0, 12.6
+    if (all_rows <= 256 || rows == 1) combine(k_packed_combine<1>, 1);
+    else if (all_rows <= 768 || rows == 2) combine(k_packed_combine<2>, 2);
     else combine(k_packed_combine<4>, 4);
   }
   return launch_check(h, "im_attn_packed_with_readout");
