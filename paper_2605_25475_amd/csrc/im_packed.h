@@ -1092,14 +1092,17 @@ __device__ __forceinline__ int pg_below(const int32_t* __restrict__ list, int n,
 
 // First launch: one workgroup.  A shared page that has a hole below n_keep is copied (a new page is taken for it, in order, as at an
 // append); pages behind n_keep are given up.  The table as it was stays in the scratch for the second launch, which moves the rows.
+#define PG_PLAN_ITEMS 4096   // up to this many (unit, page) pairs the plan's notes are in LDS: a step is a round trip less each
+#define PG_PLAN_UNITS 1024
 __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
                                                               const int32_t* __restrict__ len, const int32_t* __restrict__ evict_idx,
                                                               const int32_t* __restrict__ n_keep, const int32_t* __restrict__ n_evict,
                                                               int units, int T, int C, int max_live, PgScratch ws,
                                                               int32_t* __restrict__ status) {
-  __shared__ int s_wave[16], s_shared;
+  __shared__ int s_wave[16], s_shared, s_rank[PG_PLAN_ITEMS], s_hole[PG_PLAN_ITEMS], s_end[PG_PLAN_UNITS];
   const uint32_t tid = threadIdx.x, lane = tid & 63, items = (uint32_t)units * (uint32_t)T;
-  int32_t* hole = ws.free_ids;   // until there are ids: whether a page has a hole
+  const bool small = items <= PG_PLAN_ITEMS && units <= PG_PLAN_UNITS;
+  int32_t *rank = small ? s_rank : ws.rank, *hole = small ? s_hole : ws.free_ids, *end = small ? s_end : ws.end;   // (hole: until there are ids)
   auto lists_fit = [&](int u) {
     const int n = len[u], nk = n_keep[u], ne = n_evict[u];
     return n <= max_live && nk >= 0 && ne >= 0 && nk <= n && nk + ne == n;
@@ -1112,7 +1115,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
     const int page = table[i], nk = n_keep[u], ne = n_evict[u];
     const bool shared = lists_fit(u) && ne > 0 && (int)p * PG_SLOTS < nk && pg_is_page(page, n_pages) && refs[page] > 1;
     ws.old[i] = page;
-    ws.rank[i] = shared ? 1 : 0;
+    rank[i] = shared ? 1 : 0;
     hole[i] = 0;
     if (shared) s_shared = 1;
   }
@@ -1120,10 +1123,11 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
   int found = 0;
   const bool any_shared = s_shared != 0;
   if (any_shared) {
+#pragma unroll 2
     for (int u = tid >> 6; u < units; u += 16) {
-      if (!lists_fit(u)) continue;
-      const int32_t* evict = evict_idx + (size_t)u * C;
       const int nk = n_keep[u], ne = n_evict[u];
+      const int32_t* evict = evict_idx + (size_t)u * C;
+      if (!lists_fit(u)) continue;
       bool more = true;
       for (int e0 = 0; e0 < ne && more; e0 += 512) {
         int e[8];
@@ -1139,12 +1143,12 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
     int want = 0;
     for (uint32_t i0 = 0; i0 < items; i0 += 1024) {
       const uint32_t i = i0 + tid;
-      const int need = i < items ? ws.rank[i] & hole[i] : 0;
+      const int need = i < items ? rank[i] & hole[i] : 0;
       int total;
       const int before = pg_scan(need, s_wave, total);
       if (i < items) {
-        ws.rank[i] = need ? want + before : -1;
-        if (i % (uint32_t)T == (uint32_t)T - 1) ws.end[i / (uint32_t)T] = want + before + need;
+        rank[i] = need ? want + before : -1;
+        if (i % (uint32_t)T == (uint32_t)T - 1) end[i / (uint32_t)T] = want + before + need;
       }
       want += total;
     }
@@ -1154,8 +1158,8 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
   }
   auto enough = [&](int u) {
     if (!any_shared) return true;
-    const int end = ws.end[u], begin = u ? ws.end[u - 1] : 0;
-    return end == begin || end <= found;
+    const int e = end[u], begin = u ? end[u - 1] : 0;
+    return e == begin || e <= found;
   };
   for (int u = tid; u < units; u += 1024) {
     const bool fit = lists_fit(u), pages = enough(u);
@@ -1166,7 +1170,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
 #pragma unroll 2
   for (uint32_t i = tid; i < items; i += 1024) {
     const uint32_t u = i / (uint32_t)T, p = i - u * T;
-    const int old = ws.old[i], r = any_shared ? ws.rank[i] : -1, nk = n_keep[u];
+    const int old = ws.old[i], r = any_shared ? rank[i] : -1, nk = n_keep[u];
     const bool fit = lists_fit(u) && enough(u);
     if (old == -1 || !fit) continue;
     if (r >= 0) {
@@ -1196,7 +1200,13 @@ __global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages
   if (ne == 0) return;
   const int32_t *keep = keep_idx + (size_t)unit * C, *evict = evict_idx + (size_t)unit * C;
   const int32_t *old = ws.old + (size_t)unit * T, *tab = table + (size_t)unit * T;
-  const int stay = ne < nk ? nk - pg_below(evict, ne, nk) : pg_below(keep, nk, nk);   // kept entries below nk
+  __shared__ int s_stay;   // kept entries below nk (one wave looks: its probes are 64 cache lines each)
+  if (threadIdx.x < 64) {
+    const int found = ne < nk ? nk - pg_below(evict, ne, nk) : pg_below(keep, nk, nk);
+    if (lane == 0) s_stay = found;
+  }
+  __syncthreads();
+  const int stay = s_stay;
   const int moves = nk - stay;
   // the page that slot s was in; none for a list's entry that is no slot, or a table's that is no page
   auto page_of = [&](int s) {
