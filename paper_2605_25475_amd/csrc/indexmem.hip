@@ -124,7 +124,7 @@ bool exact_fits(const im_config* c, long long M) {
   return N > 32 && K <= XG_MAX_K && M < (1 << 30) && ((M + 15) / 16) * ((N + 15) / 16) > 2048;
 }
 
-// Records of the many-row attention over packed pages: 34 MB hold those of every launch of up to 512 workgroups
+// Records of the attention over packed pages that a handle for several queries has room for: 34 MB, those of 512 workgroups of 128 rows
 #define PG_MOST_RECS 65536
 
 size_t n_sets_of(const im_config* c) { return (size_t)c->batch * (c->head_shared ? 1 : c->n_kv_heads); }
@@ -204,9 +204,9 @@ void layout(const im_config* c, im_handle* h) {
   h->off_pgunit = take(packed, 3 * units * sizeof(int32_t));
   h->off_pgitem = take(packed, 3 * units * T * sizeof(int32_t));
   size_t queries = h->attn_chunks > 16 ? h->attn_chunks : 16;   // (records per query head)
-  if (c->max_queries > 16) {
-    const size_t many = heads * c->max_queries < PG_MOST_RECS ? c->max_queries : PG_MOST_RECS / heads;
-    if (many > queries) queries = many;
+  if (c->max_queries > 1) {   // 16 splits of every query, as far as 34 MB hold them
+    const size_t most = PG_MOST_RECS / heads, want = (size_t)c->max_queries * 16;
+    if (want > queries && most > queries) queries = want < most ? want : most;
   }
   h->pg_recs = c->head_shared ? 0 : heads * queries;
   h->off_pgrec = take(packed, h->pg_recs * PG_REC * sizeof(float));
@@ -1063,23 +1063,35 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
   a.q = (const bf16_t*)q; a.q_pos = q_pos; a.part = (float*)(h->ws + h->off_pgrec); a.status = status_ptr(h);
   a.n_pages = pk->n_pages; a.T = pg_table_pages(c); a.C = c.capacity; a.H = c.n_q_heads; a.H_kv = c.n_kv_heads; a.G = G; a.n_q = n_q;
   a.max_live = h->max_live; a.scale = c.softmax_scale;
-  const bool few = rows <= 16;   // (16 records per query head are always there)
-  const int tiles = few ? 1 : (rows + PG_ROWS - 1) / PG_ROWS, wave_pages = few ? 4 : 1;
+  // us, few rows' kernel against many rows' kernel (with the splits joined by the same launch), 4 query heads per KV head: 20 rows, 1 x 65536 entries 35 / 55, 8 x
+  // 16384 56 / 99; 36 rows 53 / 58, 93 / 99; 64 rows 58 / 73, 101 / 101, 8 x 2048 28 / 26; 96 rows 76 / 100, 193 / 104, 46 / 28
+  const bool few = rows <= 64 && room >= 1;   // (16 records per query head are always there)
+  const int tile_rows = few ? (rows <= 16 ? 16 : 32) : PG_ROWS, tiles = (rows + tile_rows - 1) / tile_rows, wave_pages = few ? 4 : 1;
   // the workgroups of one generation, two per CU.  One query over 8 units x 131072 entries, aiming at 256, 512, 768, 1024: 44.8, 37.6, 44.8, 39.8 us
   int splits = (int)((512 + (long long)tiles * units - 1) / ((long long)tiles * units));
   const int most = (n_pages + wave_pages - 1) / wave_pages;
   if (splits > most) splits = most;
-  if (splits > room) splits = room;
+  if (splits > room - !few) splits = room - !few;   // (many rows: the readout has the place of a split)
   a.n_splits = splits < 1 ? 1 : splits;
   const bf16_t *Wt = (const bf16_t*)p->Wtheta, *wg = (const bf16_t*)p->wg;
   if (few) {
-    if (q_pos) k_packed_attn_few<true><<<dim3(a.n_splits, units), 256, 0, s>>>(a);
-    else k_packed_attn_few<false><<<dim3(a.n_splits, units), 256, 0, s>>>(a);
+    const dim3 grid(a.n_splits, units, tiles);
+    if (rows <= 16) {
+      if (q_pos) k_packed_attn_few<true, 1><<<grid, 256, 0, s>>>(a);
+      else k_packed_attn_few<false, 1><<<grid, 256, 0, s>>>(a);
+    } else {
+      if (q_pos) k_packed_attn_few<true, 2><<<grid, 256, 0, s>>>(a);
+      else k_packed_attn_few<false, 2><<<grid, 256, 0, s>>>(a);
+    }
   } else {
-    const PgReadout ro = {Wt, wg, st->M, st->b, p->cg, c.mem_eps, (bf16_t*)out, readout_dbg};
+    // (behind the records, on a 16-byte boundary: a split's place has 130 floats a row)
+    float* res = a.n_splits > 1 ? a.part + (all_rows * a.n_splits * PG_REC + 3) / 4 * 4 : readout_dbg;
+    const PgReadout ro = {Wt, wg, st->M, st->b, p->cg, c.mem_eps, (bf16_t*)out, res};
     k_packed_attn_many<<<tiles * a.n_splits * units, 256, 0, s>>>(a, ro, units);
+    if (a.n_splits > 1)
+      k_packed_join<<<(unsigned)((all_rows + 1) / 2), 256, 0, s>>>(a.part, a.n_splits, all_rows, res, (bf16_t*)out, readout_dbg);
   }
-  if (few || a.n_splits > 1) {
+  if (few) {
     auto combine = [&](auto kernel, int rw) {
       kernel<<<dim3((rows + rw - 1) / rw, units), 512, 0, s>>>(a.part, a.n_splits, (const bf16_t*)q, Wt, wg, p->cg, st->M, st->b, c.n_q_heads,
                                                                c.n_kv_heads, G, n_q, c.mem_eps, (bf16_t*)out, readout_dbg);
