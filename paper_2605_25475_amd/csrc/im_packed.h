@@ -1172,15 +1172,17 @@ __device__ __forceinline__ int pg_below(const int32_t* __restrict__ list, int n,
 // append); pages behind n_keep are given up.  The table as it was stays in the scratch for the second launch, which moves the rows.
 #define PG_PLAN_ITEMS 4096   // up to this many (unit, page) pairs the plan's notes are in LDS: a step is a round trip less each
 #define PG_PLAN_UNITS 1024
+template <bool SMALL>
 __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restrict__ table, int32_t* __restrict__ refs, int n_pages,
                                                               const int32_t* __restrict__ len, const int32_t* __restrict__ evict_idx,
                                                               const int32_t* __restrict__ n_keep, const int32_t* __restrict__ n_evict,
                                                               int units, int T, int C, int max_live, PgScratch ws,
                                                               int32_t* __restrict__ status) {
-  __shared__ int s_wave[16], s_shared, s_rank[PG_PLAN_ITEMS], s_hole[PG_PLAN_ITEMS], s_end[PG_PLAN_UNITS];
+  __shared__ int s_wave[16], s_shared, s_rank[SMALL ? PG_PLAN_ITEMS : 1], s_hole[SMALL ? PG_PLAN_ITEMS : 1], s_end[SMALL ? PG_PLAN_UNITS : 1];
   const uint32_t tid = threadIdx.x, lane = tid & 63, items = (uint32_t)units * (uint32_t)T;
-  const bool small = items <= PG_PLAN_ITEMS && units <= PG_PLAN_UNITS;
-  int32_t *rank = small ? s_rank : ws.rank, *hole = small ? s_hole : ws.free_ids, *end = small ? s_end : ws.end;   // (hole: until there are ids)
+  auto rank = [&](size_t i) -> int& { if constexpr (SMALL) return s_rank[i]; else return ws.rank[i]; };
+  auto hole = [&](size_t i) -> int& { if constexpr (SMALL) return s_hole[i]; else return ws.free_ids[i]; };   // (until there are ids)
+  auto end = [&](size_t i) -> int& { if constexpr (SMALL) return s_end[i]; else return ws.end[i]; };
   auto lists_fit = [&](int u) {
     const int n = len[u], nk = n_keep[u], ne = n_evict[u];
     return n <= max_live && nk >= 0 && ne >= 0 && nk <= n && nk + ne == n;
@@ -1193,8 +1195,8 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
     const int page = table[i], nk = n_keep[u], ne = n_evict[u];
     const bool shared = lists_fit(u) && ne > 0 && (int)p * PG_SLOTS < nk && pg_is_page(page, n_pages) && refs[page] > 1;
     ws.old[i] = page;
-    rank[i] = shared ? 1 : 0;
-    hole[i] = 0;
+    rank(i) = shared ? 1 : 0;
+    hole(i) = 0;
     if (shared) s_shared = 1;
   }
   __syncthreads();
@@ -1213,7 +1215,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
         for (int j = 0; j < 16; ++j) e[j] = e0 + 64 * j + (int)lane < ne ? evict[e0 + 64 * j + lane] : nk;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          if ((uint32_t)e[j] < (uint32_t)nk) hole[(size_t)u * T + e[j] / PG_SLOTS] = 1;
+          if ((uint32_t)e[j] < (uint32_t)nk) hole((size_t)u * T + e[j] / PG_SLOTS) = 1;
         more = !__any(e[15] >= nk);
       }
     }
@@ -1221,12 +1223,12 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
     int want = 0;
     for (uint32_t i0 = 0; i0 < items; i0 += 1024) {
       const uint32_t i = i0 + tid;
-      const int need = i < items ? rank[i] & hole[i] : 0;
+      const int need = i < items ? rank(i) & hole(i) : 0;
       int total;
       const int before = pg_scan(need, s_wave, total);
       if (i < items) {
-        rank[i] = need ? want + before : -1;
-        if (i % (uint32_t)T == (uint32_t)T - 1) end[i / (uint32_t)T] = want + before + need;
+        rank(i) = need ? want + before : -1;
+        if (i % (uint32_t)T == (uint32_t)T - 1) end(i / (uint32_t)T) = want + before + need;
       }
       want += total;
     }
@@ -1236,7 +1238,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
   }
   auto enough = [&](int u) {
     if (!any_shared) return true;
-    const int e = end[u], begin = u ? end[u - 1] : 0;
+    const int e = end(u), begin = u ? end(u - 1) : 0;
     return e == begin || e <= found;
   };
   for (int u = tid; u < units; u += 1024) {
@@ -1248,7 +1250,7 @@ __global__ __launch_bounds__(1024) void k_packed_plan_compact(int32_t* __restric
 #pragma unroll 2
   for (uint32_t i = tid; i < items; i += 1024) {
     const uint32_t u = i / (uint32_t)T, p = i - u * T;
-    const int old = ws.old[i], r = any_shared ? rank[i] : -1, nk = n_keep[u];
+    const int old = ws.old[i], r = any_shared ? rank(i) : -1, nk = n_keep[u];
     const bool fit = lists_fit(u) && enough(u);
     if (old == -1 || !fit) continue;
     if (r >= 0) {

@@ -1116,8 +1116,11 @@ int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk,
   const im_config& c = h->cfg;
   const int units = c.batch * c.n_kv_heads, T = pg_table_pages(c);
   const PgScratch ws = pg_scratch(h);
-  k_packed_plan_compact<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity,
-                                           h->max_live, ws, status_ptr(h));
+  auto plan = [&](auto kernel) {
+    kernel<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity, h->max_live, ws, status_ptr(h));
+  };
+  if ((long long)units * T <= PG_PLAN_ITEMS && units <= PG_PLAN_UNITS) plan(k_packed_plan_compact<true>);
+  else plan(k_packed_plan_compact<false>);
   // a wave per 16 moved entries, and per copied page
   int gx = (h->max_live / 16 + T) / 4 + 1;
   if (gx > 64) gx = 64;

@@ -264,7 +264,7 @@ def test_a_prompt_chunk_sees_the_entries_before_it_and_itself():
     p.check()
 
 
-@pytest.mark.parametrize("n_q", [1, 20])
+@pytest.mark.parametrize("n_q", [1, 20, 50])
 def test_an_empty_cache_gives_the_readout_alone(n_q):
     p = Pair(batch=2, heads=(4, 2), capacity=70)
     p.append(5)
@@ -275,7 +275,7 @@ def test_an_empty_cache_gives_the_readout_alone(n_q):
 
 
 @pytest.mark.parametrize("scale", [1e-3, 30.0])
-@pytest.mark.parametrize("n_q", [1, 33])
+@pytest.mark.parametrize("n_q", [1, 10, 33])
 def test_flat_and_peaked_softmax(n_q, scale):
     p = Pair(batch=1, heads=(4, 2), capacity=400)
     p.append(390)
@@ -283,7 +283,7 @@ def test_flat_and_peaked_softmax(n_q, scale):
     p.attend(n_q, scale=scale)
 
 
-@pytest.mark.parametrize("n_q", [3, 40])
+@pytest.mark.parametrize("n_q", [3, 20, 40])
 def test_nan_reaches_the_queries_that_see_it_and_no_others(n_q):
     p = Pair(batch=1, heads=(4, 2), capacity=300)
     k, v = p.bf(1, 2, 280, 128), p.bf(1, 2, 280, 128)
@@ -316,7 +316,7 @@ def test_entries_beyond_the_promised_length_are_not_looked_at():
     im.im_set_max_live(p.h, 100)
     q = p.bf(1, 1, 4, 128)
     out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
-    for n_q in (1, 30):
+    for n_q in (1, 30, 50):
         x = q.expand(1, n_q, 4, 128).contiguous()
         out = torch.zeros(x.shape, dtype=torch.bfloat16, device=DEV)
         im.im_attn_packed_with_readout(p.h, p.p, p.st, x.cuda(), out)
@@ -333,7 +333,7 @@ def test_entries_beyond_the_promised_length_are_not_looked_at():
     p.check(status=im.IM_STATUS_LIVE_EXCEEDED)
 
 
-@pytest.mark.parametrize("n_q", [1, 30])
+@pytest.mark.parametrize("n_q", [1, 30, 50])
 def test_a_table_entry_that_names_no_page_is_skipped(n_q):
     p = Pair(batch=1, heads=(4, 2), capacity=300)
     p.append(290)
@@ -396,6 +396,34 @@ def test_forks_share_pages_until_one_of_them_writes():
     p.fork([-1, -1, -1, -1])
     p.check()
     assert int(p.st.refs.sum()) == 0
+
+
+def test_many_units_and_pages():
+    """More (unit, page) pairs than one pass of a plan takes, and than its notes in LDS hold."""
+    p = Pair(batch=8, heads=(8, 8), capacity=4480, n_pages=3000)
+    p.append(1030)
+    p.check()
+    p.fork([0, 0, 2, 2, -1, 5, 5, -1])
+    p.append(70)
+    p.compact(np.random.default_rng(3).integers(0, 71, (8, 8)))
+    p.check()
+    p.append(5)
+    p.check()
+
+
+def test_two_handles_take_pages_of_one_pool():
+    """Two layers' tables over one pool of pages, their calls one after another."""
+    a, b = Pair(batch=1, heads=(2, 2), capacity=200, n_pages=12), Pair(batch=1, heads=(2, 2), capacity=200, n_pages=12, seed=1)
+    b.st.pages, b.st.refs = a.st.pages, a.st.refs
+    b.st.pk = im.binding.ImPacked(a.st.pages.data_ptr(), a.st.refs.data_ptr(), b.st.table.data_ptr(), 12)
+    b.ref.refs = a.ref.refs
+    for p in (a, b, a, b):
+        p.append(60)
+        p.check()
+    a.compact(10)
+    b.append(70)
+    b.check()
+    a.check()
 
 
 def test_forks_that_are_refused_leave_their_sequences_as_they_were():
@@ -523,7 +551,7 @@ def test_calls_give_the_same_bits_each_time_on_any_stream():
 
 
 @pytest.mark.parametrize("spread", [2.0 ** 10, 2.0 ** 26, 2.0 ** 60])
-@pytest.mark.parametrize("n_q", [1, 40])
+@pytest.mark.parametrize("n_q", [1, 20, 40])
 def test_values_of_very_different_size(n_q, spread):
     """Queries that see the small values alone get them as exactly as if there were no others."""
     p = Pair(batch=1, heads=(4, 2), capacity=300)
