@@ -740,9 +740,10 @@ __device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, float 
 // P^T's registers are its operand as they are; V^T's keys are laid out in LDS in that order (16 t + 8 half + 4 g + j for key
 // 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded in LDS by the whole workgroup, between the products S^T of the page before it, and the
 // bytes of the page behind it are on their way.  (8 waves of 256 rows, half of them expanding K and half V: 470 us where this takes 473.)
-//   K goes in as bf16 (exact).  P goes in as fp16, half a step of 2^-11 off each (the sums of P stay fp32), with V as fp16 multiples of 2^e per
-// 32 dims, e the largest scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment
-// is gone over again for the scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
+//   K goes in as bf16 (exact).  2^7 P goes in as fp16, half a step of 2^-11 off each (the sums of P stay fp32), or 2^-32 where P is below 2^-21:
+// 2^17 entries of a flat tail together are 2^-15 off (without the 2^7: 2^-8).  V goes in as fp16 multiples of 2^e per 32 dims, e the largest
+// scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment is gone over again for the
+// scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
 __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout ro, int units) {
   __shared__ __attribute__((aligned(16))) char s_tile[2 * PG_TILE];
   __shared__ PgTile s_extra[2];
@@ -891,7 +892,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[d][r] *= f;
       }
-      const float mc = m * c2;
+      const float mc = fmaf(m, c2, -7.f);
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < 4; ++u) {   // 16 keys
@@ -1009,11 +1010,12 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
       segment(count, my_e, band, bands);
     }
   }
+  l = halves_sum_f(l) * 0x1p-7f;
+  const float to_o = a.n_splits > 1 ? 0x1p-7f : l == 0.f ? 0.f : 0x1p-7f / l;   // (no entry seen: 0)
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_was[d] - 127);
-  l = halves_sum_f(l);
+    for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r] * to_o, e_was[d] - 127);
 
   if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_join
     if (my_row < R) {
@@ -1031,7 +1033,6 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   // the memory readout of the wave's rows: phi^T = Wtheta Q^T, then M^T phi^T with phi and M as two bf16 parts each (2^-16).  Wtheta, then M's parts go
   // through LDS, once for the four waves (each reading them from the cache by itself: 20 us more of 16384 rows x 8 units): row r's 16-byte
   // piece g at 16 (16 r + (g ^ r % 16)), M by dims with its rows in the order of phi's registers.
-  const float inv = l == 0.f ? 0.f : 1.f / l;
   const float* Mu = ro.M + (size_t)unit * IM_DM * IM_D;
   auto piece_at = [&](int r, int g) { return s_tile + 256 * r + 16 * (g ^ (r & 15)); };
 #pragma unroll
@@ -1104,7 +1105,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           res[r] = gate * mem[4 * g + r];
-          x[r] = ((nan_blocks >> d) & 1u ? NAN : o[d][4 * g + r] * inv) + res[r];
+          x[r] = ((nan_blocks >> d) & 1u ? NAN : o[d][4 * g + r]) + res[r];
         }
         const size_t at = q_row * IM_D + 32 * d + 8 * g + 4 * half;
         if (a.n_splits == 1)

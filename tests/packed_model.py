@@ -149,7 +149,7 @@ class PackedModel(O.OracleLayer):
                 out[bi, s, hi * g:(hi + 1) * g], res[bi, s, hi * g:(hi + 1) * g] = o + gate * m, gate * m
                 # a weight exp(l - max) / sum is off by the error of its logit: fp32 sums of exact products (2^-24 of the sum of
                 # |q k| scale, a few times: below 2^-18 of it) and by fp32 exp and sums (2^-20).  Up to 16 rows a unit it goes into its
-                # product as two bf16 parts (2^-17), above as fp16: half a step of 2^-11, and of 2^-24 where it is below 2^-14.  The
+                # product as two bf16 parts (2^-17), above as fp16: half a step of 2^-11, and of 2^-31 where it is below 2^-21.  The
                 # weights sum to 1, so the output is off by that times the largest |v|.  Memory: 2^-15 of the sum of its terms (phi and M
                 # in two bf16 parts each, 2^-16; fp32 sums).  The output's rounding: half a step, 2^-9 to 2^-8 of it.
                 big = np.abs(V[seen]).max() if seen.any() and np.isfinite(V[seen]).any() else 0.0

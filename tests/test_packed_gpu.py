@@ -283,6 +283,20 @@ def test_flat_and_peaked_softmax(n_q, scale):
     p.attend(n_q, scale=scale)
 
 
+@pytest.mark.parametrize("n_q", [1, 20, 40])
+def test_a_long_flat_tail_under_one_large_weight(n_q):
+    """2^16 entries whose weights are 2^-16, 2^-22, 2^-25 or less of the largest: together they count, each by itself hardly."""
+    p = Pair(batch=1, heads=(2, 1), capacity=1 << 16)
+    for i in range(4):
+        k, v = (torch.zeros(1, 1, 1 << 14, 128).bfloat16() for _ in range(2))
+        v[...] = 1.0
+        if i == 1:
+            k[0, 0, 777], v[0, 0, 777] = 1.5, 0.0
+        p.append(1 << 14, k, v)
+    q = torch.ones(1, n_q, 2, 128) * torch.tensor([0.65, 0.9, 1.03, 1.25])[torch.arange(n_q) % 4][None, :, None, None]   # (logits of 11 to 21)
+    p.attend(n_q, q=q.bfloat16())
+
+
 @pytest.mark.parametrize("n_q", [3, 20, 40])
 def test_nan_reaches_the_queries_that_see_it_and_no_others(n_q):
     p = Pair(batch=1, heads=(4, 2), capacity=300)
