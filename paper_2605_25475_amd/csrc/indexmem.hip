@@ -1116,11 +1116,15 @@ int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk,
   const im_config& c = h->cfg;
   const int units = c.batch * c.n_kv_heads, T = pg_table_pages(c);
   const PgScratch ws = pg_scratch(h);
-  auto plan = [&](auto kernel) {
-    kernel<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity, h->max_live, ws, status_ptr(h));
-  };
-  if ((long long)units * T <= PG_PLAN_ITEMS && units <= PG_PLAN_UNITS) plan(k_packed_plan_compact<true>);
-  else plan(k_packed_plan_compact<false>);
+  if ((long long)units * T <= PG_PLAN_ITEMS && units <= PG_PLAN_UNITS) {
+    k_packed_plan_compact<<<1, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, units, T, c.capacity,
+                                             h->max_live, ws, status_ptr(h));
+  } else {
+    k_packed_plan_units<<<units, 1024, 0, s>>>(pk->table, pk->refs, pk->n_pages, st->len, evict_idx, n_keep, n_evict, T, c.capacity,
+                                               h->max_live, ws);
+    k_packed_plan_pages<<<1, 1024, 0, s>>>(pk->refs, pk->n_pages, st->len, n_keep, n_evict, units, h->max_live, ws, status_ptr(h));
+    k_packed_plan_table<<<dim3((T + 255) / 256, units), 256, 0, s>>>(pk->table, pk->refs, pk->n_pages, n_keep, T, ws);
+  }
   // a wave per 16 moved entries, and per copied page
   int gx = (h->max_live / 16 + T) / 4 + 1;
   if (gx > 64) gx = 64;

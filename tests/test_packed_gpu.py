@@ -425,6 +425,26 @@ def test_many_units_and_pages():
     p.check()
 
 
+def test_many_units_with_too_few_pages_and_lists_that_do_not_fit():
+    p = Pair(batch=8, heads=(8, 8), capacity=4480, n_pages=1200)
+    p.append(140)
+    p.fork([0, 0, 2, 2, 2, -1, 6, 6])       # 64 units of 3 pages, 8 of them empty: 72 pages in use
+    p.st.refs[172:] = 1                     # 100 are free, the rest another user's
+    p.ref.refs[172:] = 1
+    keep = np.random.default_rng(4).integers(70, 100, (8, 8))
+    keep[5] = 0
+    p.compact(keep)                         # 56 units with holes in two shared pages each: the last ones go without
+    p.check(status=16)
+    len0 = p.st.len.clone()
+    idx = torch.zeros((8, 8, 4480), dtype=torch.int32, device=DEV)
+    n_keep, n_evict = len0.clone(), torch.zeros_like(len0)
+    n_keep[3, 2], n_evict[3, 2] = -1, 141   # lists that do not fit, some of them with the right sum
+    n_keep[4, 1] += 1
+    im.im_compact_packed(p.h, p.st, idx, n_keep, idx, n_evict)
+    p.ref.status = im.IM_STATUS_BAD_LISTS
+    p.check(status=im.IM_STATUS_BAD_LISTS)
+
+
 def test_two_handles_take_pages_of_one_pool():
     """Two layers' tables over one pool of pages, their calls one after another."""
     a, b = Pair(batch=1, heads=(2, 2), capacity=200, n_pages=12), Pair(batch=1, heads=(2, 2), capacity=200, n_pages=12, seed=1)
