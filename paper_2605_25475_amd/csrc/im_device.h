@@ -28,12 +28,15 @@ __device__ __forceinline__ bf16_t f2bf_rne(float f) {
   return (bf16_t)(u >> 16);
 }
 
-// fp64 -> bf16 with ONE rounding (nearest even): truncate to fp32 with a sticky last bit
-// (round to odd), which is innocuous because fp32 carries 16 more bits than bf16, then round.
+// fp64 -> bf16 with ONE rounding (nearest even).  Rounded to fp32 first, which decides alike unless that lands half way between two bf16
+// values without being there: then it is moved to the side that x is on.
 __device__ __forceinline__ bf16_t d2bf_rne(double x) {
-  float f = __double2float_rz(x);
+  const float f = (float)x;
   uint32_t u = __float_as_uint(f);
-  if ((double)f != x) u |= 1u;
+  if ((u & 0xffffu) == 0x8000u) {
+    const double d = (double)f;
+    if (d != x) u += fabs(d) < fabs(x) ? 1u : 0xffffffffu;
+  }
   return f2bf_rne(__uint_as_float(u));
 }
 

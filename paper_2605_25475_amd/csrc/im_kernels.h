@@ -135,6 +135,15 @@ __device__ __forceinline__ double row16_sum_d(double v) {
   return v;
 }
 
+// the value of lane N of each quad
+template <int N>
+__device__ __forceinline__ double quad_lane_d(double v) {
+  const long long b = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(b & 0xffffffffll), 0x55 * N, 0xF, 0xF, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), 0x55 * N, 0xF, 0xF, false);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned int)lo);
+}
+
 __device__ __forceinline__ float row16_sum_f(float v) {
   v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, false));
   v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, false));
@@ -179,8 +188,9 @@ __device__ __forceinline__ void project_keys_rows(const uint4 (&ka)[4], bf16_t* 
         acc[cb] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)fa[e], (double)fb[e], acc[cb], 0, 0, 0);
     }
   }
-  // RMSNorm over the 64 outputs of a row: this lane's 4 columns, then the 16 lanes of its row
-  double wn[4];
+  // RMSNorm over the 64 outputs of a row: this lane's 4 columns, then the 16 lanes of its row.  Lane r of a quad takes the root and the reciprocal
+  // of row r for the quad; a quotient is the product with the reciprocal, corrected once (Markstein: the correctly rounded quotient).
+  double wn[4], mine = 1.0;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) wn[cb] = norm_w ? (double)bf2f(norm_w[16 * cb + l16]) : 1.0;
 #pragma unroll
@@ -189,10 +199,18 @@ __device__ __forceinline__ void project_keys_rows(const uint4 (&ka)[4], bf16_t* 
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb) ss = fma(acc[cb][r], acc[cb][r], ss);
     ss = row16_sum_d(ss);
-    const double rr = sqrt(ss / (double)IM_DI + (double)rms_eps);
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb) sm.outs[w][4 * r + kq][16 * cb + l16] = d2bf_rne(acc[cb][r] / rr * wn[cb]);
+    mine = (l16 & 3) == r ? ss : mine;
   }
+  const double root = sqrt(mine / (double)IM_DI + (double)rms_eps), recip = 1.0 / root;
+  const double rr[4] = {quad_lane_d<0>(root), quad_lane_d<1>(root), quad_lane_d<2>(root), quad_lane_d<3>(root)};
+  const double ri[4] = {quad_lane_d<0>(recip), quad_lane_d<1>(recip), quad_lane_d<2>(recip), quad_lane_d<3>(recip)};
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) {
+      const double q = acc[cb][r] * ri[r];
+      sm.outs[w][4 * r + kq][16 * cb + l16] = d2bf_rne(fma(fma(-q, rr[r], acc[cb][r]), ri[r], q) * wn[cb]);
+    }
   // the wave's own 16 x 64 tile goes out in 16-byte pieces (LDS operations of one wave complete in order)
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();

@@ -238,9 +238,10 @@ __global__ __launch_bounds__(256) void k_packed_append_few(char* __restrict__ pa
 
 // The same for more rows: grid (tiles of 64 new rows, units), 4 waves of 16 rows.  Lane (l16, kq) has dims 32 kq .. 32 kq + 31 of row l16, a
 // block of its own, as the key projection takes them: a row is read once, and rounded while the projection's products run.  8 units x 4096 rows:
-// 24 us, of which the fp64 projection alone takes 23 (7 at the fp64 matrix cores' peak: 512 workgroups are one generation, each a chain of
-// loads, products, norm and stores); 32 units x 4096 rows 68 us, 2.8 TB/s.  (Rounding and projection as workgroups of their own: 45 us for 8 units.)
-__global__ __launch_bounds__(256) void k_packed_append(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
+// 19 us, one generation of workgroups, each a chain of loads, products (7 us at the fp64 matrix cores' peak; without them 14 us), norm, rounding
+// and stores; 32 units x 4096 rows 59 us, 3.2 TB/s (at 3 waves per SIMD instead of 4: 61).  (Rounding and projection as workgroups of their
+// own: twice the time.)
+__global__ __launch_bounds__(256, 4) void k_packed_append(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
                                                        bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos,
                                                        const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new,
                                                        const int32_t* __restrict__ pos_new, int n_new, int H_kv, int C,
