@@ -460,6 +460,23 @@ def test_two_handles_take_pages_of_one_pool():
     a.check()
 
 
+@pytest.mark.parametrize("n_pages,free", [(37, 37), (37, 9), (1063, 40), (17000, 40)])
+def test_counts_that_start_on_any_integer(n_pages, free):
+    """Pools of any size, the free pages their last ones, their counts 4 bytes behind a 16-byte boundary."""
+    p = Pair(batch=1, heads=(2, 2), capacity=600, n_pages=n_pages)
+    p.st.refs = torch.zeros(n_pages + 1, dtype=torch.int32, device=DEV)[1:]
+    p.st.pk = im.binding.ImPacked(p.st.pages.data_ptr(), p.st.refs.data_ptr(), p.st.table.data_ptr(), n_pages)
+    p.st.refs[:n_pages - free] = 1
+    p.ref.refs[:n_pages - free] = 1
+    p.append(200)
+    p.check()
+    p.append(63)
+    p.append(100)
+    p.check(status=16 if free < 12 else 0)
+    p.compact(70)
+    p.check()
+
+
 def test_forks_that_are_refused_leave_their_sequences_as_they_were():
     p = Pair(batch=4, heads=(2, 2), capacity=100)
     p.append(90)
