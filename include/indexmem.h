@@ -348,7 +348,8 @@ int32_t im_decode_step_shared_hidden(im_handle* h, const im_params* p, const im_
  *                      -> im_compact_packed -> im_attn_packed_with_readout
  * where im_memory_update takes a state with the K, V that im_unpack_kv wrote to (buffers of one layer's size, which all layers
  * can share) and the M, b of the cache's own.
- * All of these calls return IM_ERR_UNSUPPORTED for head_shared = 1. */
+ * All of these calls return IM_ERR_UNSUPPORTED for head_shared = 1.  Rows (k_new, v_new, K_out, V_out, q, out, readout_dbg) begin on a
+ * 16-byte boundary. */
 
 /* New tokens enter the cache: the rows k_new, v_new [B, H_kv, n_new, d_head] (bf16) go, rounded to 4 bits, to slots
  * [len, len + n_new) of every unit, pos_new [B, n_new] to their positions, and Kidx = bf16(RMSNorm(Uk k_new)) (fp64 arithmetic,

@@ -236,7 +236,8 @@ bool state_ok(const im_state* st) {
 }
 // a state whose K and V rows are packed pages
 bool dense_ok(const im_state* st) { return st && st->Kidx && st->pos && st->len && st->n_projected && st->M && st->b; }
-bool packed_ok(const im_packed* pk) { return pk && pk->pages && pk->refs && pk->table && pk->n_pages >= 1 && ((uintptr_t)pk->pages & 15) == 0; }
+bool on_16(const void* p) { return ((uintptr_t)p & 15) == 0; }   // (read and written 16 bytes at a time)
+bool packed_ok(const im_packed* pk) { return pk && pk->pages && pk->refs && pk->table && pk->n_pages >= 1 && on_16(pk->pages); }
 bool params_ok(const im_params* p) { return p && p->Uq && p->G && p->Uk && p->Wtheta && p->wg; }
 
 // KV heads per set, and the number of sets (what lengths, lists and the memory state are kept per)
@@ -1005,6 +1006,7 @@ int32_t im_append_packed(im_handle* h, const im_params* p, const im_state* st, c
   IM_REQUIRE(params_ok(p), "params has a NULL pointer");
   IM_REQUIRE_PACKED();
   IM_REQUIRE(k_new && v_new && pos_new, "k_new / v_new / pos_new is NULL");
+  IM_REQUIRE(on_16(k_new) && on_16(v_new), "k_new / v_new is not on a 16-byte boundary");
   IM_REQUIRE(n_new >= 1 && n_new <= h->cfg.capacity, "n_new must be in 1..capacity");
   hipStream_t s = (hipStream_t)stream;
   int rc = ensure_ws(h, s);
@@ -1029,6 +1031,7 @@ int32_t im_unpack_kv(im_handle* h, const im_state* st, const im_packed* pk, cons
   if (!h) return IM_ERR_INVALID_ARG;
   IM_REQUIRE_PACKED();
   IM_REQUIRE(K_out && V_out, "K_out / V_out is NULL");
+  IM_REQUIRE(on_16(K_out) && on_16(V_out), "K_out / V_out is not on a 16-byte boundary");
   IM_REQUIRE((idx && n_idx) || (!idx && !n_idx), "only one of idx / n_idx is NULL");
   hipStream_t s = (hipStream_t)stream;
   int rc = ensure_ws(h, s);
@@ -1049,6 +1052,7 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
   IM_REQUIRE(params_ok(p), "params has a NULL pointer");
   IM_REQUIRE_PACKED();
   IM_REQUIRE(q && out, "q / out is NULL");
+  IM_REQUIRE(on_16(q) && on_16(out) && on_16(readout_dbg), "q / out / readout_dbg is not on a 16-byte boundary");
   IM_REQUIRE(n_q >= 1 && (long long)n_q * h->cfg.batch * h->cfg.n_q_heads < (1ll << 31), "n_q must be >= 1, and batch * n_q * n_q_heads below 2^31");
   hipStream_t s = (hipStream_t)stream;
   int rc = ensure_ws(h, s);

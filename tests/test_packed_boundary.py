@@ -71,6 +71,20 @@ def test_arguments_are_checked(name, bad):
     assert getattr(lib, name)(h, *_calls(**bad)[name]) == E
 
 
+@pytest.mark.parametrize("name,arg", [("im_append_packed", "k"), ("im_append_packed", "v"), ("im_unpack_kv", "K"), ("im_unpack_kv", "V"),
+                                      ("im_attn_packed_with_readout", "q"), ("im_attn_packed_with_readout", "out")])
+@pytest.mark.parametrize("off", [2, 8])
+def test_rows_that_begin_off_a_16_byte_boundary_are_refused(name, arg, off):
+    lib, h = _handle()
+    assert getattr(lib, name)(h, *_calls(**{arg: X + off})[name]) == E
+    assert b"boundary" in lib.im_last_error(h)
+
+
+def test_a_readout_off_a_16_byte_boundary_is_refused():
+    lib, h = _handle()
+    assert lib.im_attn_packed_with_readout(h, C.byref(PR), C.byref(ST), C.byref(PK), X, X, 1, X, X + 4, None) == E
+
+
 def test_scoring_and_selection_take_a_state_without_rows_and_the_others_do_not():
     lib, h = _handle()
     st, pr = C.byref(ST), C.byref(PR)
