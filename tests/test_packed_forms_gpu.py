@@ -1,0 +1,170 @@
+"""Attention over the cache held in 4 bits, in each of its forms (few rows of 16 and of 32, many rows with and without splits, one or
+several segments of 512 pages), against the definition in fp64 with bounds that follow the weights."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_25475_amd as im
+from helpers import f64
+from packed_model import close
+from test_packed_gpu import DEV, Pair
+
+pytestmark = pytest.mark.gpu
+
+# queries per sequence that the handle is made for, queries, heads
+FORMS = {"16 rows": (1, 4, (4, 2)), "32 rows": (64, 16, (4, 2)), "2 x 32 rows": (64, 30, (4, 2)), "many": (1, 40, (4, 2)),
+         "many, few rows": (1, 20, (4, 2)), "many, in splits": (128, 40, (4, 2)), "many, 3 tiles in splits": (128, 70, (4, 1))}
+
+
+def expect(p, q, q_pos=None, lost=None):
+    """(output, tolerance, NaN outputs) of q [B, n_q, H, 128]; lost [B, Hk, C]: entries that are not there.
+
+    A weight is off by the error of its logit (fp32 sums of exact products, exp2, its argument: below 2^-17 of the sum of |q k| scale)
+    and by its rounding: two bf16 parts (2^-17) up to 64 rows a unit on a handle that is made for them, else one fp16 value: half a step
+    of 2^-11, or 2^-32 of the largest weight where it is below 2^-21 of it.  fp32 sums of n terms, 16 in a product: (n / 16 + 64)
+    roundings of 2^-24.  The output is a quotient: twice that, of the weighted sum of |v|.  The readout is off by 2^-15 of the sum of its
+    terms, the output by half a step of its rounding, 2^-8 of it, and by 2^-122 where the scales go to their end."""
+    r, g = p.ref, p.H // p.Hk
+    B, n_q = q.shape[:2]
+    out, tol, nan = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape, bool)
+    fp16 = n_q * g > 16 and (n_q * g > 64 or p.cfg.max_queries < n_q)
+    for b in range(B):
+        for h in range(p.Hk):
+            n = int(r.len[b, h])
+            K, V = r.K[b, h, :n], r.V[b, h, :n]
+            x = q[b, :, h * g:(h + 1) * g].reshape(n_q * g, 128)
+            seen = np.ones((n_q, n), bool) if q_pos is None else r.pos[b, h, :n][None] <= np.asarray(q_pos)[b][:, None]
+            if lost is not None:
+                seen = seen & ~lost[b, h, :n]
+            seen = seen.repeat(g, 0)
+            bad = seen.astype(float) @ np.isnan(V) + (seen.astype(float) @ np.isnan(K).any(1, keepdims=True)) > 0
+            K, V = np.nan_to_num(K), np.nan_to_num(V)
+            logit = np.where(seen, x @ K.T * r.cfg.softmax_scale, -np.inf)
+            top = logit.max(1, keepdims=True, initial=-1e300)
+            w = np.exp(logit - top)
+            total = w.sum(1, keepdims=True)
+            w = w / np.where(total > 0, total, 1)
+            size = np.where(seen, np.abs(x) @ np.abs(K).T * r.cfg.softmax_scale, 0).max(1, keepdims=True, initial=0)
+            eps = (2.0 ** -12 if fp16 else 0) + 2.0 ** -16 + 2.0 ** -17 * size + (n / 16 + 64) * 2.0 ** -24
+            t = 2 * eps * (w @ np.abs(V)) + (2.0 ** -31 * (seen @ np.abs(V)) if fp16 else 0)
+            phi = x @ r.p.Wtheta.T
+            den = ((phi * phi) @ r.b[b, h] + r.cfg.mem_eps)[:, None]
+            gate = 1 / (1 + np.exp(-(x @ r.p.wg + r.p.cg)))[:, None]
+            o = w @ V + gate * (phi @ r.M[b, h]) / den
+            t = t + 2.0 ** -15 * gate * (np.abs(phi) @ np.abs(r.M[b, h])) / den + 2.0 ** -8 * np.abs(o) + 2.0 ** -122
+            sl = (b, slice(None), slice(h * g, (h + 1) * g))
+            out[sl], tol[sl], nan[sl] = (a.reshape(n_q, g, 128) for a in (o, t, bad))
+    return out, tol, nan
+
+
+def check(p, q, q_pos=None, lost=None, status=0):
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    qp = None if q_pos is None else torch.tensor(np.ascontiguousarray(q_pos), dtype=torch.int32, device=DEV)
+    im.im_attn_packed_with_readout(p.h, p.p, p.st, q.cuda(), out, qp)
+    assert im.im_query_status(p.h) == status
+    want, tol, nan = expect(p, f64(q), q_pos, lost)
+    close(f64(out), np.where(nan, np.nan, want), tol)
+
+
+def make(form, capacity, seed=0):
+    max_queries, n_q, heads = FORMS[form]
+    return Pair(batch=1, heads=heads, capacity=capacity, max_queries=max_queries, seed=seed), n_q
+
+
+def positions(n_q, n, seed=1):
+    """From nothing seen to everything."""
+    q_pos = np.random.default_rng(seed).integers(0, n, (1, n_q))
+    q_pos[0, :4] = -1, n - 1, n // 3, 0
+    return q_pos
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("scale", [1e-3, 1.0, 30.0])
+def test_flat_and_peaked_softmax(form, scale):
+    p, n_q = make(form, 700)
+    p.append(690, pos=torch.randperm(690, generator=p.g).int()[None])
+    p.memory()
+    q = p.bf(1, n_q, p.H, 128, scale=scale)
+    check(p, q)
+    check(p, q, positions(n_q, 690))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_nan_reaches_the_queries_that_see_it_and_no_others(form):
+    p, n_q = make(form, 400)
+    k, v = p.bf(1, p.Hk, 390, 128), p.bf(1, p.Hk, 390, 128)
+    v[0, 0, 100, 40] = float("nan")
+    v[0, 0, 270, 127] = float("inf")
+    v[0, 0, 388, 0] = float("nan")
+    k[0, p.Hk - 1, 330, 3] = float("-inf")
+    p.append(390, k, v, pos=torch.arange(390, dtype=torch.int32)[None])
+    p.memory()
+    q_pos = positions(n_q, 390)
+    q_pos[0, :4] = 50, 150, 389, 99
+    q = p.bf(1, n_q, p.H, 128)
+    check(p, q, q_pos)
+    check(p, q, np.full((1, n_q), 99))
+    check(p, q)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_a_table_entry_that_names_no_page_is_skipped(form):
+    p, n_q = make(form, 500)
+    p.append(490)
+    p.memory()
+    lost = np.zeros((1, p.Hk, 500), bool)
+    p.st.table[0, p.Hk - 1, 2] = -1
+    p.st.table[0, 0, 5] = 1 << 30
+    lost[0, p.Hk - 1, 128:192] = True
+    lost[0, 0, 320:384] = True
+    q = p.bf(1, n_q, p.H, 128)
+    check(p, q, lost=lost, status=im.IM_STATUS_BAD_PAGE)
+    check(p, q, positions(n_q, 490), lost=lost, status=im.IM_STATUS_BAD_PAGE)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_empty_units_and_units_of_one_entry(form):
+    p, n_q = make(form, 200)
+    p.append(130)
+    p.memory()
+    q = p.bf(1, n_q, p.H, 128)
+    for n in ([[0, 130], [1, 0], [64, 65]] if p.Hk == 2 else [[0], [1], [64]]):
+        p.set_len(torch.tensor([n]))
+        check(p, q)
+        check(p, q, positions(n_q, 130))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_entries_beyond_the_promised_length_are_not_looked_at(form):
+    p, n_q = make(form, 400)
+    p.append(390)
+    p.memory()
+    im.im_set_max_live(p.h, 150)
+    p.ref.len[:] = 150
+    q = p.bf(1, n_q, p.H, 128)
+    check(p, q, status=im.IM_STATUS_LIVE_EXCEEDED)
+    check(p, q, positions(n_q, 390), status=im.IM_STATUS_LIVE_EXCEEDED)
+
+
+# ---- more than one segment of 512 pages in one split -------------------------------------------------------------
+def long_cache(n, values, pos, seed=0):
+    """One head, and a number of queries (128 rows and more) for which a handle made for one query has records of one split: (layer, queries)."""
+    p = Pair(batch=1, heads=(1, 1), capacity=n, n_pages=(n + 63) // 64, seed=seed)
+    for i in range(0, n, 1 << 14):
+        m = min(1 << 14, n - i)
+        p.append(m, v=values[i:i + m].bfloat16()[None, None], pos=torch.as_tensor(pos[i:i + m], dtype=torch.int32)[None])
+    return p, (n + 127) // 128 // 2 + 1
+
+
+@pytest.mark.parametrize("n", [257 * 64, 300 * 64 - 5, 511 * 64 + 1, 513 * 64 - 63, 513 * 64, 700 * 64 + 9, 1031 * 64 + 1])
+def test_more_pages_than_a_wave_knows_and_than_a_segment_holds(n):
+    g = torch.Generator().manual_seed(n)
+    v = torch.randn(n, 128, generator=g)
+    order = torch.randperm((n + 63) // 64, generator=g)
+    pos = (order.repeat_interleave(64)[:n] * 64 + torch.arange(n) % 64).numpy()   # pages in no order: a mask drops some, in odd numbers
+    p, n_q = long_cache(n, v, pos, seed=n)
+    p.memory()
+    q = p.bf(1, n_q, 1, 128)
+    check(p, q)
+    check(p, q, positions(n_q, n))
+    check(p, q, np.random.default_rng(n).integers(0, 64 * 9, (1, n_q)))
