@@ -372,7 +372,7 @@ int32_t im_unpack_kv(im_handle* h, const im_state* st, const im_packed* pk, cons
  * For a chunk of a prompt: append its tokens, then attend with their positions.  n_q may be above max_queries; a handle made for
  * n_q queries has the workspace to split their entries over the whole chip.  A key or value block that reads as NaN makes
  * NaN of the outputs of the queries that see it, and of no others.  The sums are held in fp32 before they are divided: values
- * of 2^96 and above may give an infinity.  batch * n_q * H < 2^31. */
+ * of 2^96 and above may give an infinity; value blocks with no value above 6 * 2^-126 may count as 0.  batch * n_q * H < 2^31. */
 int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* q,
                                     const int32_t* q_pos, int32_t n_q, void* out, float* readout_dbg, void* stream);
 

@@ -727,9 +727,10 @@ struct PgTile {   // what goes with a tile
 };
 
 // 4 keys x 8 dims of V (a word of codes and a scale byte per key) -> 8 pieces of 4 keys, fp16 values in units of 2^(e - 127); unit = 2^(127 - e).
-// Exact for scales of e - 22 .. e (a code is at least 0.5); a scale byte of 0 gives 0.
-#define PG_BAND 23
-#define PG_BANDS 5
+// Exact for scales of e - 23 .. e + 13 (the smallest value is 0.5 x 2^-23, the largest 6 x 2^13 < 65504); a scale byte of 0 gives 0.
+#define PG_BELOW 23
+#define PG_ABOVE 13
+#define PG_BAND (PG_BELOW + PG_ABOVE + 1)
 __device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, float unit, uint2 (&piece)[8]) {
   const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w}, sc[4] = {vs << 23, (vs << 15) & 0x7f800000u, (vs << 7) & 0x7f800000u, (vs >> 1) & 0x7f800000u};
   uint32_t x[4][4];
@@ -755,9 +756,11 @@ __device__ __forceinline__ void pg_v_pieces(const uint4& vw, uint32_t vs, float 
 // 16 t + 8 g + 4 half + j).  A page of 64 keys is expanded in LDS by the whole workgroup, between the products S^T of the page before it, and the
 // bytes of the page behind it are on their way.  (8 waves of 256 rows, half of them expanding K and half V: 470 us where this takes 473.)
 //   K goes in as bf16 (exact).  2^7 P goes in as fp16, half a step of 2^-11 off each (the sums of P stay fp32), or 2^-32 where P is below 2^-21:
-// 2^17 entries of a flat tail together are 2^-15 off (without the 2^7: 2^-8).  V goes in as fp16 multiples of 2^e per 32 dims, e the largest
-// scale of the segment's entries: exact where their scales are less than 2^23 apart.  Where they are not, the segment is gone over again for the
-// scales of the next 2^23 (up to 5 times).  (V as bf16 and P as two bf16 parts: 48 products a page instead of 32.)
+// 2^17 entries of a flat tail together are 2^-15 off (without the 2^7: 2^-8).  V goes in as fp16 multiples of a power of two per 32 dims, which the
+// first segment's scales give: exact while all scales are among the 37 around it.  A segment with others is gone over once for every 37 powers of
+// two that its scales span (up to 7 times), in units of their own, and what was summed up in the units before waits in private memory, as sums of
+// the values themselves: fp32 holds these from 2^-126 up to entries of 2^96, whichever of them a row sees.  (V as bf16 and P as two bf16 parts:
+// 48 products a page instead of 32.  The products of a page from 0, added to sums of the values in the loop: 560 us instead of 488, registers.)
 //   4096 queries x 4 heads over 8 units x 8192 entries, causal: 474 us, 888 TFLOP/s of what the mask leaves (1389 in a large library product).
 // The vector instructions of the softmax and the expansion (half of the cycles) and the products (36 %) share two waves per SIMD, that 256
 // registers and the tiles allow; 56 us are the lists, the readout and the output.
@@ -796,7 +799,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
   float m = -1e30f, l = 0.f;
   uint32_t nan_blocks = 0;
-  int e_was[4] = {127, 127, 127, 127};   // o[d] counts in 2^(e_was[d] - 127)
+  int e_of[4] = {0, 0, 0, 0};   // o[d] counts 2^7 P V in 2^(e_of[d] - 127); 0: no values yet
   im_c16 o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] = pg_zero16();
@@ -819,8 +822,9 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     if (a.q_pos) ps = pos[min(p * PG_SLOTS + lane, n - 1)];
   };
 
-  // the listed pages; my_e: the units of this thread's share of V (2^(my_e - 127)); bands: times that the segment is gone over, this is the band-th
-  auto segment = [&](int count, int my_e, int band, int bands) {
+  // the listed pages; my_e: the units of this thread's share of V (2^(my_e - 127)); bands: times that the segment is gone over, this is the band-th,
+  // with the PG_BAND scales up to my_top
+  auto segment = [&](int count, int my_e, int my_top, int band, int bands) {
     const float unit = pg_scale(254 - max(my_e, 1));   // 2^(127 - my_e)
     // Entries behind the last one hold anything: their values are taken as 0, as a block of NaN is, which the rows that see it get below,
     // and what belongs to another band.  Whether there is NaN among these.
@@ -836,7 +840,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
           const uint32_t byte = (vs >> (8 * i)) & 255u;
           const bool live = 16 * w + 4 * kq + i < nk, nan = byte == 255u;
           odd |= live && nan;
-          if (!live || nan || (bands > 1 && (uint32_t)(my_e - (int)byte) >= PG_BAND)) sc &= ~(255u << (8 * i));
+          if (!live || nan || (bands > 1 && (uint32_t)(my_top - (int)byte) >= PG_BAND)) sc &= ~(255u << (8 * i));
         }
         vs = sc;
       }
@@ -943,6 +947,32 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     v_put ^= PG_TILE;
   };
 
+  // what o holds goes to the sums that wait (2^7 of P are 2^(134 - 127)), which follow the maximum.  (In memory by the compiler's own word: registers
+  // are what the loop over the pages lacks.)
+  float by_memory[65];
+  typedef __attribute__((address_space(5))) volatile float by_float;
+  by_float* by = (by_float*)by_memory;
+  bool waits = false;
+  auto put_by = [&]() {
+    if (!waits) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) by[i] = 0.f;
+      by[64] = m;
+    }
+    const float f = __builtin_amdgcn_exp2f((by[64] - m) * c2);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        by[16 * d + r] = fmaf(by[16 * d + r], f, ldexpf(o[d][r], e_of[d] - 134));
+        o[d][r] = 0.f;
+      }
+      e_of[d] = 0;
+    }
+    by[64] = m;
+    waits = true;
+  };
+
   for (int seg = p_begin; seg < p_end; seg += PG_SEG) {
     const int n_seg = min(PG_SEG, p_end - seg);
     // which pages the tile's rows see, which of them whole, and the largest and smallest scale (above 1, which is as good as 0) of their
@@ -1008,31 +1038,45 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
     if (count == 0) continue;
     int bands = 1;
     for (int band = 0; band < bands; ++band) {
-      int my_e = 127;
+      int top[4], low[4];   // the scales of the band; top -PG_BAND: there are none, all are taken as 0
+      bool fit = true;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         int hi = 0, lo = 255;
 #pragma unroll
         for (int i = 0; i < 4; ++i) { hi = max(hi, s_scale[i][d][0]); lo = min(lo, s_scale[i][d][1]); }
-        const int mine = hi > 0 ? min((hi - lo) / PG_BAND + 1, PG_BANDS) : 1;   // (what is 2^115 below the largest counts as 0)
-        bands = max(bands, mine);
-        const int e = hi > 0 ? hi - PG_BAND * min(band, mine - 1) : 127;
-        if (d == l16 >> 2) my_e = band < mine ? e : -PG_BAND;   // (a block without scales in this band: all are taken as 0)
-        if (e != e_was[d]) {   // o goes over to these units
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r], e_was[d] - e);
-          e_was[d] = e;
-        }
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        bands = hi > 0 ? max(bands, (hi - lo) / PG_BAND + 1) : bands;
+        top[d] = hi - PG_BAND * band;
+        if (hi == 0 || top[d] < lo) top[d] = -PG_BAND;
+        low[d] = max(lo, top[d] - PG_BAND + 1);
+        fit = fit && (top[d] < 0 || e_of[d] == 0 || (top[d] <= e_of[d] + PG_ABOVE && low[d] >= e_of[d] - PG_BELOW));
       }
-      segment(count, my_e, band, bands);
+      if (!fit) put_by();
+#pragma unroll
+      for (int d = 0; d < 4; ++d)   // (the first units leave room for larger scales to come, where they can)
+        if (top[d] > 0 && e_of[d] == 0) e_of[d] = max(top[d] - (top[d] - low[d] < PG_BAND - 6 ? PG_ABOVE - 6 : PG_ABOVE), 1);
+      const int my_d = l16 >> 2, my_e = my_d & 2 ? (my_d & 1 ? e_of[3] : e_of[2]) : (my_d & 1 ? e_of[1] : e_of[0]);
+      const int my_top = my_d & 2 ? (my_d & 1 ? top[3] : top[2]) : (my_d & 1 ? top[1] : top[0]);
+      segment(count, my_e > 0 ? my_e : 127, my_top, band, bands);   // (no units: what is there is 0, or as good as 0)
+    }
+  }
+  if (waits) {
+    put_by();
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = by[16 * d + r];
+      e_of[d] = 134;
     }
   }
   l = halves_sum_f(l) * 0x1p-7f;
-  const float to_o = a.n_splits > 1 ? 0x1p-7f : l == 0.f ? 0.f : 0x1p-7f / l;   // (no entry seen: 0)
+  const float to_o = a.n_splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (no entry seen: 0)
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r] * to_o, e_was[d] - 127);
+    for (int r = 0; r < 16; ++r) o[d][r] = ldexpf(o[d][r] * to_o, e_of[d] - 134);
 
   if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_join
     if (my_row < R) {

@@ -146,6 +146,27 @@ def test_entries_beyond_the_promised_length_are_not_looked_at(form):
     check(p, q, positions(n_q, 390), status=im.IM_STATUS_LIVE_EXCEEDED)
 
 
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("power", [10, 26, 45, 70, 110, 180])
+@pytest.mark.parametrize("large_first", [False, True])
+def test_values_of_very_different_size(form, power, large_first):
+    """Queries that see the small values alone get them as exactly as if there were no others."""
+    p, n_q = make(form, 400)
+    v = p.bf(1, p.Hk, 390, 128).float()
+    small = torch.arange(390) < 200
+    v[:, :, ~small if large_first else small] *= 2.0 ** -min(power, 100)
+    if power > 100:
+        v[:, :, small if large_first else ~small] *= 2.0 ** (power - 100)
+    v[:, :, 30, 32:64] *= 2.0 ** -4
+    pos = torch.arange(390, dtype=torch.int32)
+    p.append(390, v=v.bfloat16(), pos=(389 - pos if large_first else pos)[None].contiguous())
+    q = p.bf(1, n_q, p.H, 128)
+    first = 189 if large_first else 199        # (the last position of the small values)
+    check(p, q, np.full((1, n_q), first))
+    check(p, q, np.linspace(0, 389, n_q).astype(int)[None])
+    check(p, q)
+
+
 # ---- more than one segment of 512 pages in one split -------------------------------------------------------------
 def long_cache(n, values, pos, seed=0):
     """One head, and a number of queries (128 rows and more) for which a handle made for one query has records of one split: (layer, queries)."""
@@ -168,3 +189,38 @@ def test_more_pages_than_a_wave_knows_and_than_a_segment_holds(n):
     check(p, q)
     check(p, q, positions(n_q, n))
     check(p, q, np.random.default_rng(n).integers(0, 64 * 9, (1, n_q)))
+
+
+@pytest.mark.parametrize("powers", [(0, -40), (0, -100), (0, -104), (0, -110), (0, -123), (-123, 0), (-60, 40), (40, -123, 0), (90, -30)])
+def test_segments_of_very_different_size(powers):
+    """A segment after another whose values are far larger or smaller: the sums over the first stay, and queries that see the second
+    alone get it exactly."""
+    n = 512 * 64 * len(powers) - 64 * 511 - 63    # the last segment has one entry
+    at = torch.arange(n) // (512 * 64)
+    v = torch.ones(n, 128) * 2.0 ** torch.tensor(powers, dtype=torch.float64)[at].float()[:, None]
+    v[:, 32:64] *= 1.5 * (1 - 2 * (torch.arange(n) % 3 == 0).float())[:, None]
+    v[:, 64:96] = torch.where(at[:, None] == len(powers) - 1, v[:, 64:96], torch.zeros(1))
+    p, n_q = long_cache(n, v, (n - 1 - torch.arange(n)).numpy())
+    q = p.bf(1, n_q, 1, 128, scale=1e-2)
+    check(p, q)
+    check(p, q, np.zeros((1, n_q), int))
+    q_pos = np.linspace(0, n - 1, n_q).astype(int)[None]
+    q_pos[0, 1] = 1
+    check(p, q, q_pos)
+
+
+def test_bands_within_and_between_segments():
+    """Small and large values side by side in the first segment, the large ones alone in the second, the small ones alone in the third."""
+    n = 1024 * 64 + 70
+    g = torch.Generator().manual_seed(5)
+    v = torch.randn(n, 128, generator=g)
+    i = torch.arange(n)
+    small = ((i < 32768) & (i % 3 == 0)) | (i >= 65536)
+    v = torch.where(small[:, None], v * 2.0 ** -90, v)
+    v[17, :] *= 2.0 ** 60
+    pos = torch.where(small, i, i + n)
+    p, n_q = long_cache(n, v, pos.numpy())
+    q = p.bf(1, n_q, 1, 128)
+    check(p, q)
+    check(p, q, np.full((1, n_q), n - 1))
+    check(p, q, np.linspace(0, 2 * n, n_q).astype(int)[None])
