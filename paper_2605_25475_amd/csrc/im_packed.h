@@ -319,6 +319,13 @@ struct PgAttn {
   float scale;
 };
 #define PG_REC (IM_D + 2)
+#define PG_NO_MAX (-3e38f)   // the maximum of a row that has seen nothing: below it no entry is told from none
+
+// m c2, the reference of a row's weights exp2(s c2 - m c2): its rounding is a factor of all of them, and goes out in the quotient.  Where the
+// logits are so far from 0 that the factor leaves the weights' range (2^22: it is 2^(1/4) at most), pg_far is true, and s - m, which is exact for
+// those that count, takes the place of s
+__device__ __forceinline__ float pg_reference(float m, float c2) { return fmaxf(m * c2, PG_NO_MAX); }
+__device__ __forceinline__ bool pg_far(float m, float mc) { return m > PG_NO_MAX && fabsf(mc) > 0x1p22f; }
 
 // p[block][tile][r] of 32 keys (row 16 block + l16, key 16 tile + 4 kq + r) times V; the probabilities go in as two bf16 parts (16 bits:
 // 2^-17 of each, where one part would cost as much as the output's own rounding), o accumulates in fp32
@@ -384,7 +391,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_few(PgAttn a) {
   im_c4 o[NB][8];
 #pragma unroll
   for (int x = 0; x < NB; ++x) {
-    m[x] = -1e30f;
+    m[x] = PG_NO_MAX;
     l[x] = 0.f;
     nan_blocks[x] = 0;
 #pragma unroll
@@ -476,14 +483,30 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_few(PgAttn a) {
         }
       }
     }
+    float mc[NB];
+    bool far = false;
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
-      const float mc = m[x] * c2;
+      mc[x] = pg_reference(m[x], c2);
+      far |= pg_far(m[x], mc[x]);
+    }
+    if (__any(far)) {
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        mc[x] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[x][t][r] -= m[x];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[x][t][r] = __builtin_amdgcn_exp2f(fmaf(s[x][t][r], c2, -mc));
+          s[x][t][r] = __builtin_amdgcn_exp2f(fmaf(s[x][t][r], c2, -mc[x]));
           l[x] += s[x][t][r];
         }
     }
@@ -543,7 +566,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_few(PgAttn a) {
 #pragma unroll
   for (int x = 0; x < NB; ++x) {
     l[x] = rows_sum_f(l[x]);
-    if (kq == 0) { s_ml[w][16 * x + l16][0] = m[x] * c2; s_ml[w][16 * x + l16][1] = l[x]; s_nan[w][16 * x + l16] = nan_blocks[x]; }
+    if (kq == 0) { s_ml[w][16 * x + l16][0] = pg_reference(m[x], c2); s_ml[w][16 * x + l16][1] = l[x]; s_nan[w][16 * x + l16] = nan_blocks[x]; }
     if (R > 16 * x) att_store(o[x], &s_acc[w][16 * x][0], l16, kq, min(R - 16 * x, 16));
   }
   __syncthreads();
@@ -598,7 +621,7 @@ __global__ __launch_bounds__(512) void k_packed_combine(const float* __restrict_
 #pragma unroll
   for (int i = 0; i < RW; ++i) {
     const float* rec = part + row_of(i) * n_splits * PG_REC;
-    float m = -1e30f, l = 0.f, o = 0.f;
+    float m = PG_NO_MAX, l = 0.f, o = 0.f;
     for (int c0 = g; c0 < n_splits; c0 += 32) {   // 8 splits at a time
       float cm[8], cl[8], co[8], top = m;
 #pragma unroll
@@ -797,7 +820,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   for (int i = 1; i < 4; ++i) { q_lo = min(q_lo, s_lim[i][0]); q_hi = max(q_hi, s_lim[i][1]); }
   const int32_t *tab = a.table + (size_t)unit * a.T, *pos = a.pos + (size_t)unit * a.C;
   const float c2 = a.scale * 1.44269504088896340736f;   // exp(scale x) = exp2(c2 x)
-  float m = -1e30f, l = 0.f;
+  float m = PG_NO_MAX, l = 0.f;
   uint32_t nan_blocks = 0;
   int e_of[4] = {0, 0, 0, 0};   // o[d] counts 2^7 P V in 2^(e_of[d] - 127); 0: no values yet
   im_c16 o[4];
@@ -913,7 +936,14 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[d][r] *= f;
       }
-      const float mc = fmaf(m, c2, -7.f);
+      float mc = pg_reference(m, c2) - 7.f;
+      if (__any(pg_far(m, mc))) {
+        mc = -7.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[u][r] -= m;
+      }
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < 4; ++u) {   // 16 keys
@@ -1081,7 +1111,7 @@ __global__ __launch_bounds__(256, 2) void k_packed_attn_many(PgAttn a, PgReadout
   if (a.n_splits > 1) {   // the row's record; the splits are joined by k_packed_join
     if (my_row < R) {
       float* rec = a.part + (q_row * a.n_splits + split) * PG_REC;
-      if (half == 0) { rec[0] = m * c2; rec[1] = l; }
+      if (half == 0) { rec[0] = pg_reference(m, c2); rec[1] = l; }
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -1187,7 +1217,7 @@ __global__ __launch_bounds__(256) void k_packed_join(const float* __restrict__ p
   if (row >= rows) return;
   const float* rec = part + row * n_splits * PG_REC;
   const float r = res[row * IM_D + x];
-  float m = -1e30f, l = 0.f, o = 0.f;
+  float m = PG_NO_MAX, l = 0.f, o = 0.f;
   for (int c0 = 0; c0 < n_splits; c0 += 8) {   // 8 splits at a time
     float cm[8], cl[8], co[8], top = m;
 #pragma unroll

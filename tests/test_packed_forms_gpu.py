@@ -167,6 +167,26 @@ def test_values_of_very_different_size(form, power, large_first):
     check(p, q)
 
 
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("size", [2.0 ** 11, 2.0 ** 13, 2.0 ** 55, -2.0 ** 13, -2.0 ** 55])
+def test_logits_far_from_zero(form, size):
+    """Logits of 10^7 to 10^34 and of both signs (whole multiples of one number): the largest of them share the weight."""
+    p, n_q = make(form, 400)
+    k = torch.full((1, p.Hk, 390, 128), size)
+    first = torch.arange(390) % 5 == 0
+    k[:, :, ~first if size < 0 else first] *= 1.5
+    v = p.bf(1, p.Hk, 390, 128)
+    p.append(390, k=k.bfloat16(), v=v)
+    q = (abs(size) * (1 + torch.arange(n_q) / 128)[None, :, None, None]).expand(1, n_q, p.H, 128).bfloat16()
+    for n in (390, 1):
+        q_pos = None if n == 390 else np.zeros((1, n_q), int)
+        out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
+        im.im_attn_packed_with_readout(p.h, p.p, p.st, q.cuda(), out, None if n == 390 else torch.zeros((1, n_q), dtype=torch.int32, device=DEV))
+        rows = p.ref.V[0, :, :n][:, first.numpy()[:n]]
+        want = np.broadcast_to(rows.mean(1).repeat(p.H // p.Hk, 0)[None, None], q.shape)   # (no memory: the readout is 0)
+        close(f64(out), want, 2.0 ** -11 * np.abs(rows).mean() + 2.0 ** -8 * np.abs(want))
+
+
 # ---- more than one segment of 512 pages in one split -------------------------------------------------------------
 def long_cache(n, values, pos, seed=0):
     """One head, and a number of queries (128 rows and more) for which a handle made for one query has records of one split: (layer, queries)."""
