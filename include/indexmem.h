@@ -344,10 +344,11 @@ int32_t im_decode_step_shared_hidden(im_handle* h, const im_params* p, const im_
 
 /* ---- the cache held in 4 bits, in pages (im_packed) --------------------------------------------------------------
  * A step on it is
- *     im_append_packed -> im_index_score -> im_topb_select -> im_unpack_kv (evicted rows) -> im_memory_update
- *                      -> im_compact_packed -> im_attn_packed_with_readout
+ *     im_append_packed -> im_index_score -> im_topb_select -> im_unpack_kv (evicted rows) -> im_compact_packed
+ *                      -> im_memory_update -> im_attn_packed_with_readout
  * where im_memory_update takes a state with the K, V that im_unpack_kv wrote to (buffers of one layer's size, which all layers
- * can share) and the M, b of the cache's own.
+ * can share) and the M, b of the cache's own.  It comes behind the compaction, which may have to leave a unit as it was: it sets
+ * that unit's n_evict to 0, so that the memory does not take entries that stay in the cache.
  * All of these calls return IM_ERR_UNSUPPORTED for head_shared = 1.  Rows (k_new, v_new, K_out, V_out, q, out, readout_dbg) begin on a
  * 16-byte boundary. */
 
@@ -378,10 +379,11 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
 
 /* im_compact_kv for this cache: kept entries in slots >= n_keep move into the evicted slots < n_keep, both in ascending order
  * (their codes as they are); len = n_projected = n_keep; pages behind the last kept entry are given up.  A shared page that gets
- * entries is copied first; a unit whose copies are not all among the free pages is left as it was (IM_STATUS_OUT_OF_PAGES).  Pages that
- * the call gives up are free for the calls after it. */
+ * entries is copied first; a unit whose copies are not all among the free pages is left as it was (IM_STATUS_OUT_OF_PAGES).  n_evict of
+ * every unit that is left as it was (for its lists or its length, too) becomes 0: calls that share lists (layers that use one
+ * selection) need a copy of it each.  Pages that the call gives up are free for the calls after it. */
 int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* keep_idx, const int32_t* n_keep,
-                          const int32_t* evict_idx, const int32_t* n_evict, void* stream);
+                          const int32_t* evict_idx, int32_t* n_evict, void* stream);
 
 /* Sequences fork, and end: src_of [B] int32.  src_of[b] = b: sequence b stays as it is.  src_of[b] = a, with src_of[a] = a: b
  * becomes a copy of a; the pages are held by both, Kidx, pos, M and b are copied, and what b held before is given up.

@@ -395,6 +395,7 @@ def im_attn_packed_with_readout(h: Handle, p: Params, st: PackedState, q, out, q
 
 
 def im_compact_packed(h: Handle, st: PackedState, keep_idx, n_keep, evict_idx, n_evict) -> None:
+    """n_evict becomes 0 where the unit had to be left as it was."""
     h.check(h.lib.im_compact_packed(h.h, C.byref(st.c), C.byref(st.pk), _ptr(keep_idx), _ptr(n_keep), _ptr(evict_idx), _ptr(n_evict),
                                     _stream()))
 

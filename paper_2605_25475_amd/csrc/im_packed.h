@@ -1451,11 +1451,13 @@ __global__ __launch_bounds__(256) void k_packed_plan_table(int32_t* __restrict__
 __global__ __launch_bounds__(256) void k_packed_compact(char* __restrict__ pages, int n_pages, const int32_t* __restrict__ table, int T,
                                                         bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos, int32_t* __restrict__ len,
                                                         int32_t* __restrict__ n_projected, const int32_t* __restrict__ keep_idx,
-                                                        const int32_t* __restrict__ n_keep, const int32_t* __restrict__ evict_idx,
-                                                        const int32_t* __restrict__ n_evict, int C, PgScratch ws,
+                                                        const int32_t* n_keep, const int32_t* __restrict__ evict_idx, int32_t* n_evict, int C, PgScratch ws,
                                                         int32_t* __restrict__ status) {
   const int unit = blockIdx.y, lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), waves = gridDim.x * 4;
-  if (!ws.base[unit]) return;
+  if (!ws.base[unit]) {   // (a unit that is left as it was has evicted nothing; the plan has read its counts)
+    if (blockIdx.x == 0 && threadIdx.x == 0) n_evict[unit] = 0;
+    return;
+  }
   const int nk = n_keep[unit], ne = n_evict[unit];
   if (blockIdx.x == 0 && threadIdx.x == 0) len[unit] = n_projected[unit] = nk;
   if (ne == 0) return;

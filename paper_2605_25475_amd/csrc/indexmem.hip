@@ -1111,7 +1111,7 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
 }
 
 int32_t im_compact_packed(im_handle* h, const im_state* st, const im_packed* pk, const int32_t* keep_idx, const int32_t* n_keep,
-                          const int32_t* evict_idx, const int32_t* n_evict, void* stream) {
+                          const int32_t* evict_idx, int32_t* n_evict, void* stream) {
   if (!h) return IM_ERR_INVALID_ARG;
   IM_REQUIRE_PACKED();
   IM_REQUIRE(keep_idx && n_keep && evict_idx && n_evict, "a list pointer is NULL");

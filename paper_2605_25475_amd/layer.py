@@ -129,13 +129,14 @@ class PackedLayer:
         return out
 
     def compress(self, q_win, x_gate_win, q_pos_win, budget, lam, eta):
-        """score -> select -> evicted rows -> memory update -> compact."""
+        """score -> select -> evicted rows -> compact -> memory update.  (A unit that cannot be compacted, for want of pages, keeps its
+        entries: the compaction sets its n_evict to 0, and the memory takes none of them.)"""
         h, p, st = self.h, self.p, self.st
         B.im_index_score(h, p, st, q_win, x_gate_win, q_pos_win, self.scores)
         B.im_topb_select(h, self.scores, st, budget, self.keep_idx, self.evict_idx, self.n_keep, self.n_evict)
         B.im_unpack_kv(h, st, *self.rows, self.evict_idx, self.n_evict)
-        B.im_memory_update(h, p, self.evicted_rows, self.evict_idx, self.n_evict, lam, eta)
         B.im_compact_packed(h, st, self.keep_idx, self.n_keep, self.evict_idx, self.n_evict)
+        B.im_memory_update(h, p, self.evicted_rows, self.evict_idx, self.n_evict, lam, eta)
 
     def step(self, k_new, v_new, pos_new, q_new, x_gate, q_pos, q_attn, out, budget, lam, eta, readout=None):
         """The step of Layer.step on this cache."""

@@ -244,3 +244,42 @@ def test_bands_within_and_between_segments():
     check(p, q)
     check(p, q, np.full((1, n_q), n - 1))
     check(p, q, np.linspace(0, 2 * n, n_q).astype(int)[None])
+
+
+# ---- an event that finds no pages ---------------------------------------------------------------------------------
+def test_an_event_without_pages_for_a_units_copies_leaves_its_memory_alone():
+    """Sequences share pages and the pool is full: the unit that cannot be compacted keeps its entries, and its memory has not taken
+    them; the other unit's event happens."""
+    p = Pair(batch=2, heads=(1, 1), capacity=200, n_pages=4, max_queries=2, n_sink=2)
+    p.append(100)                           # two pages each
+    p.memory()
+    p.fork([0, 0])                          # two shared pages, two free ones
+    p.check()
+    lay, r, lam, eta = p.gpu, p.ref, float(np.float32(0.9)), 0.5
+    p.st.refs[3] = p.ref.refs[3] = 1        # and one of these another user's
+    before = f64(p.st.M), f64(p.st.b)
+    q = p.bf(2, 2, 1, 128)
+    x, pos = q.reshape(2, 2, -1), np.tile(np.arange(98, 100), (2, 1))
+    lay.compress(q.cuda(), x.cuda(), torch.tensor(pos, dtype=torch.int32, device=DEV), 60, lam, eta)
+    kept, gone = r.topb_select(r.index_score(f64(q), f64(x), pos), 60)
+    needs = [len({int(s) // 64 for s in gone[b][0] if s < 60}) for b in range(2)]
+    assert needs == [1, 1]                  # (each has holes in its first page alone: the first gets the free page)
+    r.memory_update([gone[0], [gone[1][0][:0]]], lam, eta)
+    r.compact_kv(kept, gone)
+    p.check(status=im.IM_STATUS_OUT_OF_PAGES)
+    assert p.ref.len.ravel().tolist() == [60, 100]
+    for name, was in zip(("M", "b"), before):
+        got, want = f64(getattr(p.st, name)), getattr(r, name)
+        assert np.array_equal(got[1], was[1])
+        assert np.abs(got[0] - want[0]).max() <= 1e-4 * np.sqrt((want[0] ** 2).mean())
+    # with pages, the next event takes them, once
+    p.st.refs[3] = p.ref.refs[3] = 0
+    r.status = 0
+    lay.compress(q.cuda(), x.cuda(), torch.tensor(pos, dtype=torch.int32, device=DEV), 60, lam, eta)
+    kept, gone = r.topb_select(r.index_score(f64(q), f64(x), pos), 60)
+    r.memory_update(gone, lam, eta)
+    r.compact_kv(kept, gone)
+    p.check()
+    for name in ("M", "b"):
+        got, want = f64(getattr(p.st, name)), getattr(r, name)
+        assert np.abs(got - want).max() <= 1e-4 * np.sqrt((want ** 2).mean())
