@@ -198,7 +198,7 @@ int32_t im_append_kv_hidden(im_handle* h, const im_params* p, const im_state* st
  * q_new [B, n_q, H, d_head] bf16; x_gate [B, n_q, gate_in_dim] bf16; q_pos [B, n_q] int32;
  * scores_out [B, H_kv, C] fp32, written for slots < len only.  1 <= n_q <= max_queries.
  * All arithmetic that feeds the stored bf16 / fp32 values is fp64.
- * st->K = NULL (a cache in 4 bits; its keys were projected at the append): (i) is skipped.
+ * st->K and st->V NULL (a cache in 4 bits; its keys were projected at the append; head_shared = 0): (i) is skipped.
  * head_shared = 1: (i) is skipped (the keys were made at the append), x_gate holds the queries'
  * hidden states, and scores_out is [B, C]: one score per token of the sequence. */
 int32_t im_index_score(im_handle* h, const im_params* p, const im_state* st, const void* q_new,

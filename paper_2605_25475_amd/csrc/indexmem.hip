@@ -236,6 +236,8 @@ bool state_ok(const im_state* st) {
 }
 // a state whose K and V rows are packed pages
 bool dense_ok(const im_state* st) { return st && st->Kidx && st->pos && st->len && st->n_projected && st->M && st->b; }
+// what scores and selection look at: a whole state, or that of a cache in 4 bits, without rows (per-unit layout only)
+bool scored_ok(const im_handle* h, const im_state* st) { return state_ok(st) || (dense_ok(st) && !st->K && !st->V && !h->cfg.head_shared); }
 bool on_16(const void* p) { return ((uintptr_t)p & 15) == 0; }   // (read and written 16 bytes at a time)
 bool packed_ok(const im_packed* pk) { return pk && pk->pages && pk->refs && pk->table && pk->n_pages >= 1 && on_16(pk->pages); }
 bool params_ok(const im_params* p) { return p && p->Uq && p->G && p->Uk && p->Wtheta && p->wg; }
@@ -575,7 +577,7 @@ int32_t im_index_score(im_handle* h, const im_params* p, const im_state* st, con
                        void* stream) {
   if (!h) return IM_ERR_INVALID_ARG;
   IM_REQUIRE(params_ok(p), "params has a NULL pointer");
-  IM_REQUIRE(dense_ok(st), "state has a NULL pointer");
+  IM_REQUIRE(scored_ok(h, st), "state has a NULL pointer");
   IM_REQUIRE(q_new && x_gate && q_pos && scores_out, "q_new / x_gate / q_pos / scores_out is NULL");
   IM_REQUIRE(n_q >= 1 && n_q <= h->cfg.max_queries, "n_q must be in 1..max_queries");
   hipStream_t s = (hipStream_t)stream;
@@ -663,7 +665,7 @@ int32_t im_topb_select(im_handle* h, const float* scores, const im_state* st, in
                        int32_t* keep_idx, int32_t* evict_idx, int32_t* n_keep, int32_t* n_evict,
                        void* stream) {
   if (!h) return IM_ERR_INVALID_ARG;
-  IM_REQUIRE(dense_ok(st), "state has a NULL pointer");
+  IM_REQUIRE(scored_ok(h, st), "state has a NULL pointer");
   IM_REQUIRE(scores && keep_idx && evict_idx && n_keep && n_evict, "an array pointer is NULL");
   IM_REQUIRE(budget >= h->cfg.n_sink + h->cfg.n_recent, "budget is below n_sink + n_recent");
   IM_REQUIRE(budget <= h->cfg.capacity, "budget exceeds capacity");

@@ -112,3 +112,16 @@ def test_the_models_rounding():
     ties[:8] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, -5]
     assert list(quantise(ties)[:8]) == [6, 0, 1, 1, 2, 2, 4, -4]
     assert np.isnan(quantise(np.full(128, np.inf))).all() and (quantise(np.zeros(128)) == 0).all()
+
+
+def test_scoring_and_selection_refuse_a_state_with_half_of_its_rows_and_shared_heads_without_any():
+    lib, h = _handle()
+    _, shared = _handle(head_shared=1, idx_dim=16)
+    pr = C.byref(PR)
+    for handle, st in ((h, B.ImState(None, X, *[X] * 6)), (h, B.ImState(X, None, *[X] * 6)), (shared, ST),
+                       (shared, B.ImState(None, X, *[X] * 6)), (shared, B.ImState(X, None, *[X] * 6))):
+        # (n_q and the budget are wrong as well, so that nothing is enqueued whatever is looked at)
+        assert lib.im_index_score(handle, pr, C.byref(st), X, X, X, 0, X, None) == E
+        assert b"state" in lib.im_last_error(handle)
+        assert lib.im_topb_select(handle, X, C.byref(st), 513, X, X, X, X, None) == E
+        assert b"state" in lib.im_last_error(handle)
