@@ -202,7 +202,8 @@ __device__ __forceinline__ void project_keys_rows(const uint4 (&ka)[4], bf16_t* 
     mine = (l16 & 3) == r ? ss : mine;
   }
   const double root = sqrt(mine / (double)IM_DI + (double)rms_eps), recip = 1.0 / root;
-  const double rr[4] = {quad_lane_d<0>(root), quad_lane_d<1>(root), quad_lane_d<2>(root), quad_lane_d<3>(root)};
+  const double bound = fmin(root, 0x1.fffffffffffffp1023);   // (an infinite norm: finite / inf stays 0 in the correction)
+  const double rr[4] = {quad_lane_d<0>(bound), quad_lane_d<1>(bound), quad_lane_d<2>(bound), quad_lane_d<3>(bound)};
   const double ri[4] = {quad_lane_d<0>(recip), quad_lane_d<1>(recip), quad_lane_d<2>(recip), quad_lane_d<3>(recip)};
 #pragma unroll
   for (int r = 0; r < 4; ++r)

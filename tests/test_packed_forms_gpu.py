@@ -283,3 +283,15 @@ def test_an_event_without_pages_for_a_units_copies_leaves_its_memory_alone():
     for name in ("M", "b"):
         got, want = f64(getattr(p.st, name)), getattr(r, name)
         assert np.abs(got - want).max() <= 1e-4 * np.sqrt((want ** 2).mean())
+
+
+# ---- indexer keys -------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_new", [3, 20, 70])
+def test_an_infinite_projection_weight_makes_nan_of_its_own_column_alone(n_new):
+    """The norm is infinite: what is finite becomes 0, as the quotient has it, however many rows a call projects."""
+    p = Pair(heads=(4, 2), capacity=100)
+    for row, dim, w in ((5, 7, np.inf), (9, 100, -np.inf)):
+        p.p.Uk[row, dim] = p.ref.p.Uk[row, dim] = w
+    p.append(n_new)
+    p.check()
+    assert np.isnan(p.ref.Kidx[0, :, :n_new][..., [5, 9]]).all() and (p.ref.Kidx[0, :, :n_new, :5] == 0).all()
