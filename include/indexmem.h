@@ -131,7 +131,9 @@ typedef struct im_state {
  * scales (byte 8448 + 64 (r / 16) + 16 (r % 16 / 4) + 4 c + r % 4).  136 bytes per entry, where bf16 rows take 512.
  *   Slot i of a unit lies in row i % IM_PAGE_SLOTS of page table[b, h, i / IM_PAGE_SLOTS].  Units may hold pages together
  * (im_fork_packed); refs counts a page's holders, 0 is a free page.  A call that writes to a page that others hold too takes a
- * new one and copies it first.  A new pool has refs 0 and table -1 everywhere.  New pages are the free ones of the lowest
+ * new one and copies it first (where all its holders write in one call, each of them does, and the old page goes free).  Several
+ * handles may use one pool; calls that take or give up pages of it (append, compact, fork) must then follow one another in stream
+ * order: two at once would take the same free pages.  A new pool has refs 0 and table -1 everywhere.  New pages are the free ones of the lowest
  * numbers, in the order of the units and their slots.
  *   The caller may set a len (and n_projected) to a smaller value, e.g. to drop rejected draft tokens: pages behind it
  * stay with the unit, and later appends fill them. */
@@ -371,7 +373,8 @@ int32_t im_unpack_kv(im_handle* h, const im_state* st, const im_packed* pk, cons
  * sequence: query s sees the entries with pos <= q_pos[b, s] (q_pos NULL: all of them); one that sees none has o_attn = 0.
  * q, out [B, n_q, H, d_head] bf16; q_pos [B, n_q] int32 or NULL; readout_dbg [B, n_q, H, d_head] fp32 or NULL.
  * For a chunk of a prompt: append its tokens, then attend with their positions.  n_q may be above max_queries; a handle made for
- * n_q queries has the workspace to split their entries over the whole chip.  A key or value block that reads as NaN makes
+ * n_q queries has the workspace to split their entries over the whole chip.  (One made for one query has records for
+ * max(16, ceil(capacity / 128)) splits of a query: with n_q above that, the kernel of many rows takes the entries in one piece.)  A key or value block that reads as NaN makes
  * NaN of the outputs of the queries that see it, and of no others.  The sums are held in fp32 before they are divided: values
  * of 2^96 and above may give an infinity; value blocks with no value above 6 * 2^-126 may count as 0.  batch * n_q * H < 2^31. */
 int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_state* st, const im_packed* pk, const void* q,

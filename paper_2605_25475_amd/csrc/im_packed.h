@@ -239,7 +239,8 @@ __global__ __launch_bounds__(256) void k_packed_append_few(char* __restrict__ pa
 // The same for more rows: grid (tiles of 64 new rows, units), 4 waves of 16 rows.  Lane (l16, kq) has dims 32 kq .. 32 kq + 31 of row l16, a
 // block of its own, as the key projection takes them: a row is read once, and rounded while the projection's products run.  8 units x 4096 rows:
 // 19 us, one generation of workgroups, each a chain of loads, products (7 us at the fp64 matrix cores' peak; without them 14 us), norm, rounding
-// and stores; 32 units x 4096 rows 59 us, 3.2 TB/s (at 3 waves per SIMD instead of 4: 61).  (Rounding and projection as workgroups of their
+// and stores; 32 units x 4096 rows 59 us, 3.2 TB/s (at 3 waves per SIMD instead of 4: 61, though at 4 the compiler spills 5 registers of a
+// lane, 24 bytes).  (Rounding and projection as workgroups of their
 // own: twice the time.)
 __global__ __launch_bounds__(256, 4) void k_packed_append(char* __restrict__ pages, const int32_t* __restrict__ table, int T,
                                                        bf16_t* __restrict__ Kidx, int32_t* __restrict__ pos,
@@ -361,7 +362,8 @@ __device__ __forceinline__ void pg_pv(const float (&p)[NB][2][4], const uint4 (&
 // for each block of 16 rows (keys x rows; row r is query r / G, head r % G), the softmax against a running maximum, P V.  A page is expanded once
 // for the NB blocks, in registers: its layout is that of the products' operands.  The waves' sums meet in LDS.
 //   One query of 4 heads over 8 units x 131072 entries: 31 us, 4.6 TB/s, bound by memory (a copy reaches 5.1).  16 units x 7 heads x 2048: 9.4 us.
-// With 32 rows (NB 2) the products and the softmax are in front: 20 rows over 8 x 16384 56 us.
+// With 32 rows (NB 2) the products and the softmax are in front: 20 rows over 64 units x 16384 entries 56 us.  Two blocks' logits, sums and queries and the next
+// page's bytes are more than 256 registers: the compiler spills 22 of a lane with the mask (92 bytes), 6 without (28).
 template <bool MASK, int NB>
 __global__ __launch_bounds__(256, 2) void k_packed_attn_few(PgAttn a) {
   __shared__ float s_ml[4][16 * NB][2];

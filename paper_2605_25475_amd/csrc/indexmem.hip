@@ -199,12 +199,14 @@ void layout(const im_config* c, im_handle* h) {
   h->off_xk = take(step, c->head_shared ? B * c->capacity * IM_DI_SHARED * sizeof(double) : 0);
   h->off_dpick = take(step, sets * ((c->capacity + 15) / 16) * sizeof(uint4));
   h->off_darrived = take(step, DEC_LINE * sets * sizeof(int32_t));
-  // the cache in 4 bits (PgScratch; then, in calls of their own, the attention records: one per row and split, pg_splits)
+  // the cache in 4 bits (PgScratch; then, in calls of their own, the attention records: one per row and split).  A query head has 16, as many as
+  // the dense attention has chunks, or for several queries up to 16 per query as far as 34 MB hold them, whichever is most: with long caches and
+  // many heads the chunks decide (16 x 32 heads x 131072 entries: 273 MB, as the dense attention's own records)
   const size_t T = (c->capacity + PG_SLOTS - 1) / PG_SLOTS, heads = B * c->n_q_heads;
   h->off_pgunit = take(packed, 3 * units * sizeof(int32_t));
   h->off_pgitem = take(packed, 3 * units * T * sizeof(int32_t));
   size_t queries = h->attn_chunks > 16 ? h->attn_chunks : 16;   // (records per query head)
-  if (c->max_queries > 1) {   // 16 splits of every query, as far as 34 MB hold them
+  if (c->max_queries > 1) {
     const size_t most = PG_MOST_RECS / heads, want = (size_t)c->max_queries * 16;
     if (want > queries && most > queries) queries = want < most ? want : most;
   }
@@ -1069,9 +1071,11 @@ int32_t im_attn_packed_with_readout(im_handle* h, const im_params* p, const im_s
   a.q = (const bf16_t*)q; a.q_pos = q_pos; a.part = (float*)(h->ws + h->off_pgrec); a.status = status_ptr(h);
   a.n_pages = pk->n_pages; a.T = pg_table_pages(c); a.C = c.capacity; a.H = c.n_q_heads; a.H_kv = c.n_kv_heads; a.G = G; a.n_q = n_q;
   a.max_live = h->max_live; a.scale = c.softmax_scale;
-  // us, few rows' kernel against many rows' kernel (with the splits joined by the same launch), 4 query heads per KV head: 20 rows, 1 x 65536 entries 35 / 55, 8 x
+  // us of the first launch, few rows' kernel against many rows' kernel, 4 query heads per KV head: 20 rows, 1 x 65536 entries 35 / 55, 8 x
   // 16384 56 / 99; 36 rows 53 / 58, 93 / 99; 64 rows 58 / 73, 101 / 101, 8 x 2048 28 / 26; 96 rows 76 / 100, 193 / 104, 46 / 28
-  const bool few = rows <= 64 && room >= 1;   // (16 records per query head are always there)
+  // (Every query head has 16 records at least: room for up to 16 queries whatever the handle was made for.  Above, a handle made for fewer queries may
+  // have none, and the many rows' kernel takes the call, which needs none for one split.)
+  const bool few = rows <= 64 && room >= 1;
   const int tile_rows = few ? (rows <= 16 ? 16 : 32) : PG_ROWS, tiles = (rows + tile_rows - 1) / tile_rows, wave_pages = few ? 4 : 1;
   // the workgroups of one generation, two per CU.  One query over 8 units x 131072 entries, aiming at 256, 512, 768, 1024: 44.8, 37.6, 44.8, 39.8 us
   int splits = (int)((512 + (long long)tiles * units - 1) / ((long long)tiles * units));
